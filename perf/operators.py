@@ -402,8 +402,7 @@ def _own(S):
                                normalize=c["normalize"], scale=c["scale"])
         return S["d_logits"]
     if op == "rows":
-        ciera.quantize_rows_t(S["x"], S["q"], S["s"], source=S["source"],
-                              top_k=c["k"])
+        ciera.quantize_rows_t(S["x"], S["q"], S["s"], position=S["position"])
         return [S["q"], S["s"]]
     if op == "blocks":
         ciera.quantize_blocks_t(S["w"], S["q"], S["s"], S.get("qt"),
