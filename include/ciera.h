@@ -326,6 +326,202 @@ int ciera_should_compress(const ciera_shard_stats *stats,
 int ciera_select(const double *gain, const double *mem, uint64_t count,
                  double budget_bytes, uint32_t flags, uint8_t *selected);
 
+/* ------------------------------------------------- the experts' products ----
+ * What an MoE layer does with its decoded weights: choose experts for every
+ * token (ciera_route), sort the chosen (token, slot) pairs by expert
+ * (ciera_route_plan), bring tokens and weights into an 8-bit format
+ * (ciera_quantize_*), multiply every expert's rows by its weight
+ * (ciera_expert_matmul), and add a token's rows up again (ciera_combine);
+ * with the backward pass of each.
+ *
+ * The conventions above hold: device memory owned by the caller, checks on the
+ * host, kernels enqueued on `stream` and nothing allocated, freed or
+ * synchronised, so that every call can be captured in a HIP graph. The stream
+ * has to belong to the current device. Outputs must not overlap inputs. Sizes of
+ * zero enqueue nothing unless stated. Wide values are bf16, fp16 or fp32
+ * (ciera_dtype); their pointers are aligned to the value, row strides are in
+ * values and at least the row's length. Device indices out of range are never
+ * followed. Sums are held in fp32; every result is rounded to its type once, to
+ * nearest even, and depends on the inputs alone (no atomic adds).
+ *
+ * 8-bit format: e4m3 values (OCP: no infinities, largest 448) with one scale
+ * per block of 128 values (128 x 128 for weights), a power of two 2^e held as
+ * the byte e + 127. e is the smallest integer >= -127 with amax <= 448 * 2^e,
+ * amax over the block's finite values; 0 if amax is 0. A value x is held as x *
+ * 2^-e rounded to nearest even; infinities and NaN become NaN. Scaling by a
+ * power of two is exact, so a value's only error is e4m3's half step, and the
+ * matrix cores apply the scales themselves. The contracted dimension of an 8-bit
+ * matrix is filled up with zeros to a multiple of 128 (the quantising calls
+ * write these), its row stride in bytes is a multiple of 16, its pointer
+ * 16-byte aligned; scale rows hold one byte per block, their pointer and stride
+ * are multiples of 4, and the quantising calls fill a row's last dword with 127.
+ */
+enum ciera_dtype { CIERA_DT_BF16 = 0, CIERA_DT_FP16 = 1, CIERA_DT_FP32 = 2 };
+
+#define CIERA_MAX_EXPERTS 1024u
+#define CIERA_MAX_TOP_K 64u
+#define CIERA_MAX_GROUPS 64u
+
+#define CIERA_ROUTE_SIGMOID 0x1u   /* scores sigmoid(l), else softmax(l) */
+#define CIERA_ROUTE_NORMALIZE 0x2u /* a token's weights are divided by their sum */
+#define CIERA_ROUTE_GROUP_TOP_TWO 0x4u /* a group ranks by the sum of its two
+                                 highest values (one, if it has one), else by
+                                 its highest */
+
+/* Experts for every token, from logits [n_tokens, n_experts].
+ *   score  s_e = softmax(l)_e or sigmoid(l_e)
+ *   value  v_e = s_e + bias_e (bias may be NULL: 0), by which experts are chosen
+ *   groups n_groups runs of n_experts / n_groups experts; only the top_groups
+ *          groups that rank highest take part (n_groups 1, top_groups 1: all)
+ *   choice the top_k highest values, in falling order; among equals the lowest
+ *          index, for groups too
+ *   weight scale * s_e, with CIERA_ROUTE_NORMALIZE scale * s_e / sum of the
+ *          chosen scores; the bias never enters
+ * A logit of -inf and a bias that is not finite take the expert out of the
+ * choice (with such a bias it still counts in the softmax). Slots that no expert is left
+ * for hold id -1 and weight 0; a token with a logit that is NaN or +inf has ids
+ * -1 and weights NaN. Values are compared as if computed in 64 bits: fp32
+ * values closer than their error are computed again in fp64. Without a bias (and
+ * without CIERA_ROUTE_GROUP_TOP_TWO where groups are left out) the logits
+ * themselves are compared.
+ *   expert_ids, weights   [n_tokens, top_k], int32 and fp32, contiguous.
+ * n_experts <= CIERA_MAX_EXPERTS, n_groups divides it and is at most
+ * CIERA_MAX_GROUPS, top_k <= CIERA_MAX_TOP_K and <= the experts of top_groups
+ * groups (else CIERA_EINVAL); n_tokens * top_k < 2^31. */
+int ciera_route(const void *logits, uint32_t dtype, uint64_t n_tokens,
+                uint32_t n_experts, uint64_t row_stride, const float *bias,
+                uint32_t n_groups, uint32_t top_groups, uint32_t top_k,
+                uint32_t flags, float scale, int32_t *expert_ids,
+                float *weights, hipStream_t stream);
+
+/* Gradient of the weights -> gradient of the logits, the choice held constant:
+ * d_logits [n_tokens, n_experts] is written whole, in the logits' type. ids out of
+ * range add nothing; an id that a token holds twice counts twice. flags:
+ * CIERA_ROUTE_SIGMOID, CIERA_ROUTE_NORMALIZE, as in the forward call. */
+int ciera_route_backward(const void *logits, uint32_t dtype,
+                         uint64_t n_tokens, uint32_t n_experts,
+                         uint64_t row_stride, uint32_t top_k, uint32_t flags,
+                         float scale, const int32_t *expert_ids,
+                         const float *d_weights, void *d_logits,
+                         uint64_t d_row_stride, hipStream_t stream);
+
+/* Workspace bytes of ciera_route_plan (host): 0 for sizes that it refuses. */
+uint64_t ciera_plan_workspace_bytes(uint64_t n_tokens, uint32_t top_k,
+                                    uint32_t n_experts);
+
+/* The (token, slot) pairs, numbered token * top_k + slot, sorted by expert; those
+ * of one expert keep their order. Experts are first_expert ... first_expert +
+ * n_experts - 1 (those that this rank holds); pairs of other ids are left out.
+ *   offsets   [n_experts + 1] int32: rows of expert e are offsets[e] ...
+ *             offsets[e + 1] - 1, offsets[0] = 0
+ *   source    [n_tokens * top_k] int32: the pair behind each row; -1 from row
+ *             offsets[n_experts] on
+ *   position  [n_tokens, top_k] int32: the row of each pair, -1 if left out
+ * With no tokens offsets is set to 0. The workspace needs no preparation and is
+ * free again when the call's kernels are done. */
+int ciera_route_plan(const int32_t *expert_ids, uint64_t n_tokens,
+                     uint32_t top_k, uint32_t first_expert,
+                     uint32_t n_experts, int32_t *offsets, int32_t *source,
+                     int32_t *position, void *workspace,
+                     uint64_t workspace_bytes, hipStream_t stream);
+
+/* Rows of 8-bit values with a scale per 1 x 128 block. x [n_rows, n_cols]. With
+ * `position` ([n_rows, top_k] int32) row r goes to each row position[r, s] of
+ * q, which has q_rows rows; positions outside it are skipped, and no row of
+ * q may be named twice. Without it (NULL, top_k 1) row r goes to row r. Rows of q that no
+ * position names are left as they were. q rows: n_cols values and zeros
+ * up to a multiple of 128. */
+int ciera_quantize_rows(const void *x, uint32_t dtype, uint64_t n_rows,
+                        uint64_t n_cols, uint64_t row_stride,
+                        const int32_t *position, uint32_t top_k,
+                        uint64_t q_rows, void *q, uint64_t q_stride,
+                        uint8_t *scales, uint64_t scale_stride,
+                        hipStream_t stream);
+
+/* Weights in 8 bits with a scale per 128 x 128 block. w: `batch` matrices
+ * [n_rows, n_cols], contiguous rows, one after the other.
+ *   q        batch x n_rows rows of n_cols values (filled up), q_stride apart
+ *   scales   batch x ceil(n_rows / 128) rows of ceil(n_cols / 128) bytes
+ *   q_t, scales_t   the same of the transposed matrices (the operand of the data
+ *            gradient): n_cols rows of n_rows values each; both NULL: not written */
+int ciera_quantize_blocks(const void *w, uint32_t dtype, uint64_t batch,
+                          uint64_t n_rows, uint64_t n_cols, void *q,
+                          uint64_t q_stride, uint8_t *scales,
+                          uint64_t scale_stride, void *q_t,
+                          uint64_t qt_stride, uint8_t *scales_t,
+                          uint64_t scale_t_stride, hipStream_t stream);
+
+/* Columns that ciera_quantize_columns needs at most (host), a multiple of 128:
+ * every expert's rows are filled up to a multiple of 128. */
+uint64_t ciera_columns_length(uint64_t n_rows, uint32_t n_experts);
+
+/* The transpose of an expert's rows in 8 bits with a scale per 128 rows of one
+ * column: the operands of ciera_expert_weight_grad. x [n_x, n_cols]; row p of the
+ * n_rows sorted rows is row source[p] / top_k of x (source NULL: row p; n_x ==
+ * n_rows). offsets [n_experts + 1] int32 as of ciera_route_plan. Expert e's rows
+ * become q_t[c, start_e + i], start_e the sum of its predecessors' rows, each
+ * rounded up to 128; zeros fill the last block. q_t has n_cols rows of `length` >=
+ * ciera_columns_length() columns (a multiple of 128), contiguous; scales has
+ * scale_stride >= length / 128 bytes a row. Columns and scales behind the last
+ * expert's are left as they were. */
+int ciera_quantize_columns(const void *x, uint32_t dtype, uint64_t n_x,
+                           uint64_t n_rows, uint64_t n_cols,
+                           uint64_t row_stride, const int32_t *source,
+                           uint32_t top_k, const int32_t *offsets,
+                           uint32_t n_experts, void *q_t, uint64_t length,
+                           uint8_t *scales, uint64_t scale_stride,
+                           hipStream_t stream);
+
+/* out[p, n] = sum over j of a[p, j] b[e, n, j] for the rows p of expert e
+ * (offsets[e] <= p < offsets[e + 1]), values times scales: a [n_rows, depth]
+ * 8-bit rows (1 x 128), b n_experts 8-bit matrices [n_out, depth] (128 x 128)
+ * one after the other, depth a multiple of 128 (and <= 2^23). offsets NULL: one
+ * expert with all rows. out [n_rows, n_out] of out_dtype; rows outside every
+ * expert are left as they were. offsets must not fall. With the transposed weights
+ * and the output's gradient in 8-bit rows this is the data gradient. */
+int ciera_expert_matmul(const void *a, uint64_t a_stride,
+                        const uint8_t *a_scales, uint64_t a_scale_stride,
+                        uint64_t n_rows, const void *b, uint64_t b_stride,
+                        const uint8_t *b_scales, uint64_t b_scale_stride,
+                        uint32_t n_experts, uint64_t n_out, uint64_t depth,
+                        const int32_t *offsets, void *out,
+                        uint32_t out_dtype, uint64_t out_stride,
+                        hipStream_t stream);
+
+/* Weight gradients d_w[e, n, c] = sum over the rows p of expert e of dy[p, n]
+ * x[p, c], from ciera_quantize_columns of dy and x with the same offsets and
+ * length. d_w [n_experts, n_out, n_cols] of out_dtype, contiguous; an expert
+ * without rows gets zeros. Nothing behind column `length` is read. */
+int ciera_expert_weight_grad(const void *dy_t, const uint8_t *dy_scales,
+                             uint64_t dy_scale_stride, const void *x_t,
+                             const uint8_t *x_scales,
+                             uint64_t x_scale_stride, uint64_t length,
+                             uint32_t n_experts, uint64_t n_out,
+                             uint64_t n_cols, const int32_t *offsets,
+                             void *d_w, uint32_t out_dtype,
+                             hipStream_t stream);
+
+/* out[t] = sum over s of weights[t, s] * rows[position[t, s]] in the order of s;
+ * positions outside [0, n_rows) add nothing. weights NULL: all 1 (the backward
+ * pass of giving a token to several experts). A weight that is NaN makes
+ * the token NaN whatever its position. out in the rows' type. */
+int ciera_combine(const void *rows, uint32_t dtype, uint64_t n_rows,
+                  uint64_t n_cols, uint64_t row_stride, const float *weights,
+                  const int32_t *position, uint64_t n_tokens, uint32_t top_k,
+                  void *out, uint64_t out_stride, hipStream_t stream);
+
+/* Backward pass of ciera_combine: d_rows[position[t, s]] = weights[t, s] *
+ * d_out[t] and d_weights[t, s] = <d_out[t], rows[position[t, s]]> (0 where the
+ * position is outside). No row may be named twice; rows that none names are
+ * left as they were. d_rows in the rows' type, its stride d_row_stride. */
+int ciera_combine_backward(const void *d_out, uint64_t d_out_stride,
+                           const void *rows, uint32_t dtype, uint64_t n_rows,
+                           uint64_t n_cols, uint64_t row_stride,
+                           const float *weights, const int32_t *position,
+                           uint64_t n_tokens, uint32_t top_k, void *d_rows,
+                           uint64_t d_row_stride, float *d_weights,
+                           hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

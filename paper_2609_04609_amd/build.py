@@ -16,7 +16,8 @@ LIB = os.path.join(PKG, "libciera.so")
 PROBE_LIB = os.path.join(PKG, "libciera_probe.so")
 PROBE_SOURCE = "stream_probe.hip"
 SOURCES = ["ciera_kernels.hip", "ciera_ans.hip", "ciera_api.cpp",
-           "ciera_select.cpp"]
+           "ciera_select.cpp", "ciera_route.hip", "ciera_quantize.hip",
+           "ciera_matmul.hip", "ciera_combine.hip", "ciera_expert_api.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 # Packed-fp32 instructions are disabled for every device compile: the codec
