@@ -32,12 +32,16 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-// 16 bytes a lane from global memory into LDS at `to` + 16 * lane; `to` is the
-// same for the whole wave.
+// BYTES (4 or 16) a lane from global memory into LDS at `to` + BYTES * lane;
+// `to` is the same for the whole wave.
+template <int BYTES>
 __device__ __forceinline__ void load_to_lds(const uint8_t *from, uint8_t *to) {
-  __builtin_amdgcn_global_load_lds(
-      (const __attribute__((address_space(1))) void *)from,
-      (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+  const auto global = (const __attribute__((address_space(1))) void *)from;
+  const auto local = (__attribute__((address_space(3))) void *)to;
+  if constexpr (BYTES == 16)
+    __builtin_amdgcn_global_load_lds(global, local, 16, 0, 0);
+  else
+    __builtin_amdgcn_global_load_lds(global, local, 4, 0, 0);
 }
 
 // Tiles in LDS: rows of 128 bytes in eight 16-byte chunks, chunk c of row r at
@@ -85,11 +89,13 @@ __device__ __forceinline__ Wide widen(const i32x8 &f, int scale_byte) {
   return r;
 }
 
-// What a workgroup multiplies: `steps` blocks of 128.
+// A tile's rows of an operand, from its first block on.
 struct Operand {
-  const uint8_t *data;  // block 0 of row 0
-  uint64_t stride;      // bytes a row
-  uint32_t rows;        // rows there are; later ones repeat the last
+  const uint8_t *data;    // block 0 of row 0
+  uint64_t stride;        // bytes a row
+  const uint8_t *scales;  // of row 0, the dword that holds block 0's
+  uint64_t scale_stride;  // a multiple of 4
+  uint32_t rows;          // rows there are; later ones repeat the last
 };
 
 template <typename T>
@@ -109,15 +115,33 @@ __device__ __forceinline__ void store_four(void *out, uint64_t at, uint32_t n,
   }
 }
 
-// A TR x TC tile by four waves, 2 x 2. Two stages in LDS: the loads of a block
-// are in flight while the one before is multiplied. row_scale(f, kb) and
-// col_scale(g, kb): the scale bytes of this lane's row in fragments f, g.
-template <bool EXACT, int TR, int TC, typename RS, typename CS>
-__device__ __forceinline__ void multiply(
-    const Operand &rows, const Operand &cols, uint32_t steps, uint8_t *lds,
-    RS row_scale, CS col_scale, f32x4 (&acc)[TR / 32][TC / 32]) {
-  constexpr int FR = TR / 32, FC = TC / 32;  // fragments of a wave
-  constexpr int LR = TR / 32, LC = TC / 32;  // load instructions of a wave
+// A tile of a result: TR x TC by WR x WC waves, a wave's part FR x FC fragments.
+template <int TR_, int TC_, int WR_, int WC_>
+struct Shape {
+  static constexpr int TR = TR_, TC = TC_, WR = WR_, WC = WC_;
+  static constexpr int kWaves = WR * WC, kThreads = 64 * kWaves;
+  static constexpr int PR = TR / WR, PC = TC / WC;  // a wave's rows and columns
+  static constexpr int FR = PR / 16, FC = PC / 16;
+  // load instructions (eight rows each) of a wave for a block
+  static constexpr int LR = TR / 8 / kWaves, LC = TC / 8 / kWaves;
+  static constexpr int kStage = (TR + TC) * 128;  // bytes
+  static constexpr int kScales = (TR + TC) * 4;   // a dword a row: four blocks
+  static constexpr int kLds = 2 * (kStage + kScales);
+};
+
+// Sum over `steps` blocks. Two stages in LDS: the loads of a block are in flight
+// while the one before is multiplied. Scales come by dwords, four blocks of a
+// row, into LDS as well: read where they are used they would be one cache line a
+// row and block, more of the cache's time than the values take (801 us against
+// 459 without scales, 8192 x 8192 x 8192 in 256 x 256 tiles). COL_BLOCKS: a
+// scale of the columns operand belongs to 128 rows. `phase`: the place of block 0
+// in its dword.
+template <bool EXACT, bool COL_BLOCKS, typename S>
+__device__ __forceinline__ void multiply(const Operand &rows,
+                                         const Operand &cols, uint32_t phase,
+                                         uint32_t steps, uint8_t *lds,
+                                         f32x4 (&acc)[S::FR][S::FC]) {
+  constexpr int FR = S::FR, FC = S::FC, LR = S::LR, LC = S::LC;
   const uint32_t lane = threadIdx.x & 63;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint8_t *from_r[LR], *from_c[LC];
@@ -136,35 +160,68 @@ __device__ __forceinline__ void multiply(
                 (((lane & 7) ^ ((r >> 1) & 7)) << 4);
   }
   const auto fetch = [&](uint32_t kb, uint32_t stage) {
-    uint8_t *to = lds + stage * (TR + TC) * 128;
+    uint8_t *to = lds + stage * S::kStage;
 #pragma unroll
     for (int i = 0; i < LR; ++i)
-      load_to_lds(from_r[i] + uint64_t(kb) * 128, to + (wave * LR + i) * 1024);
-    to += TR * 128;
+      load_to_lds<16>(from_r[i] + uint64_t(kb) * 128,
+                      to + (wave * LR + i) * 1024);
+    to += S::TR * 128;
 #pragma unroll
     for (int i = 0; i < LC; ++i)
-      load_to_lds(from_c[i] + uint64_t(kb) * 128, to + (wave * LC + i) * 1024);
+      load_to_lds<16>(from_c[i] + uint64_t(kb) * 128,
+                      to + (wave * LC + i) * 1024);
   };
-  int sr[FR], sc[FC], next_r[FR], next_c[FC];
+  // 64 rows' dwords an instruction; wave w has rows 64 w on of both operands
+  // after each other
+  constexpr int LS = (S::TR + S::TC) / 64;
+  const uint8_t *from_s[(LS + S::kWaves - 1) / S::kWaves];
 #pragma unroll
-  for (int f = 0; f < FR; ++f) sr[f] = row_scale(f, 0);
+  for (int i = 0; i * S::kWaves < LS; ++i) {
+    const uint32_t r = (i * S::kWaves + wave) * 64 + lane;
+    const bool is_row = r < S::TR;
+    const Operand &o = is_row ? rows : cols;
+    uint32_t held = is_row ? r : r - S::TR;
+    if (held >= o.rows) held = o.rows - 1;
+    if (COL_BLOCKS && !is_row) held /= 128;
+    from_s[i] = o.scales + held * o.scale_stride;
+  }
+  uint8_t *const scales = lds + 2 * S::kStage;
+  const auto fetch_scales = [&](uint32_t group) {
 #pragma unroll
-  for (int g = 0; g < FC; ++g) sc[g] = col_scale(g, 0);
+    for (int i = 0; i * S::kWaves < LS; ++i)
+      if (i * S::kWaves + wave < LS)
+        load_to_lds<4>(from_s[i] + uint64_t(group) * 4,
+                       scales + (group & 1) * S::kScales +
+                           (i * S::kWaves + wave) * 256);
+  };
+  fetch_scales(0);
   fetch(0, 0);
   __syncthreads();
-  const uint32_t row0 = (wave >> 1) * (TR / 2) + (lane & 15);
-  const uint32_t col0 = (wave & 1) * (TC / 2) + (lane & 15);
+  const uint32_t row0 = (wave / S::WC) * S::PR + (lane & 15);
+  const uint32_t col0 = (wave % S::WC) * S::PC + (lane & 15);
   const uint32_t quarter = lane >> 4;
+  uint32_t four_r[FR], four_c[FC];
   for (uint32_t kb = 0; kb < steps; ++kb) {
+    const uint32_t at = phase + kb;
+    if (kb == 0 || (at & 3) == 0) {
+      const uint32_t *from = reinterpret_cast<const uint32_t *>(
+          scales + ((at >> 2) & 1) * S::kScales);
+#pragma unroll
+      for (int f = 0; f < FR; ++f) four_r[f] = from[row0 + 16 * f];
+#pragma unroll
+      for (int g = 0; g < FC; ++g) four_c[g] = from[S::TR + col0 + 16 * g];
+    }
     if (kb + 1 < steps) {
-#pragma unroll
-      for (int f = 0; f < FR; ++f) next_r[f] = row_scale(f, kb + 1);
-#pragma unroll
-      for (int g = 0; g < FC; ++g) next_c[g] = col_scale(g, kb + 1);
+      if (((at + 1) & 3) == 0) fetch_scales((at + 1) >> 2);
       fetch(kb + 1, (kb + 1) & 1);
     }
-    const uint8_t *tr = lds + (kb & 1) * (TR + TC) * 128;
-    const uint8_t *tc = tr + TR * 128;
+    int sr[FR], sc[FC];
+#pragma unroll
+    for (int f = 0; f < FR; ++f) sr[f] = (four_r[f] >> (8 * (at & 3))) & 0xFF;
+#pragma unroll
+    for (int g = 0; g < FC; ++g) sc[g] = (four_c[g] >> (8 * (at & 3))) & 0xFF;
+    const uint8_t *tr = lds + (kb & 1) * S::kStage;
+    const uint8_t *tc = tr + S::TR * 128;
     if constexpr (EXACT) {
       Wide fr[FR];
 #pragma unroll
@@ -194,29 +251,26 @@ __device__ __forceinline__ void multiply(
       }
     }
     __syncthreads();
-#pragma unroll
-    for (int f = 0; f < FR; ++f) sr[f] = next_r[f];
-#pragma unroll
-    for (int g = 0; g < FC; ++g) sc[g] = next_c[g];
   }
 }
 
-// Rows r0 ... of a tile's result, columns c0 ...
-template <int TR, int TC, typename T>
-__device__ __forceinline__ void store_tile(const f32x4 (&acc)[TR / 32][TC / 32],
+// The tile's rows below `rows` and columns below n_cols - col, at row `row` and
+// column `col` of the result.
+template <typename S, typename T>
+__device__ __forceinline__ void store_tile(const f32x4 (&acc)[S::FR][S::FC],
                                            void *out, uint64_t stride,
                                            uint64_t row, uint32_t rows,
                                            uint32_t col, uint32_t n_cols,
                                            bool whole) {
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
-  for (int f = 0; f < TR / 32; ++f) {
-    const uint32_t r = (wave >> 1) * (TR / 2) + 16 * f + (lane & 15);
+  for (int f = 0; f < S::FR; ++f) {
+    const uint32_t r = (wave / S::WC) * S::PR + 16 * f + (lane & 15);
     if (r >= rows) continue;
 #pragma unroll
-    for (int g = 0; g < TC / 32; ++g) {
+    for (int g = 0; g < S::FC; ++g) {
       const uint32_t c =
-          col + (wave & 1) * (TC / 2) + 16 * g + (lane >> 4) * 4;
+          col + (wave % S::WC) * S::PC + 16 * g + (lane >> 4) * 4;
       if (c < n_cols)
         store_four<T>(out, (row + r) * stride + c, n_cols - c, whole,
                       acc[f][g]);
@@ -224,41 +278,34 @@ __device__ __forceinline__ void store_tile(const f32x4 (&acc)[TR / 32][TC / 32],
   }
 }
 
-constexpr int kTile = 128;
-
 // Grid: tiles of the result's columns, then of the experts' rows.
-template <typename T>
-__global__ void __launch_bounds__(256)
+template <typename S, typename T>
+__global__ void __launch_bounds__(S::kThreads)
     expert_matmul_kernel(MatmulArgs a, uint32_t col_tiles, bool whole) {
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * kTile * 128];
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[S::kLds];
   const uint32_t lane = threadIdx.x & 63;
   const uint32_t tile = blockIdx.x / col_tiles;
-  const uint32_t col = (blockIdx.x % col_tiles) * kTile;
-  ExpertTile where{0, tile * kTile, uint32_t(a.n_rows)};
+  const uint32_t col = (blockIdx.x % col_tiles) * S::TC;
+  ExpertTile where{0, tile * S::TR, uint32_t(a.n_rows)};
   if (a.offsets)
-    where = find_tile(a.offsets, a.n_experts, uint32_t(a.n_rows), tile, 7, lane);
+    where = find_tile(a.offsets, a.n_experts, uint32_t(a.n_rows), tile,
+                      __builtin_ctz(S::TR), lane);
   if (where.expert == kNoExpert) return;
   const uint32_t held = where.end - where.first;
   const Operand rows{a.a + uint64_t(where.first) * a.a_stride, a.a_stride,
-                     held < kTile ? held : kTile};
+                     a.a_scales + uint64_t(where.first) * a.a_scale_stride,
+                     a.a_scale_stride, held < S::TR ? held : S::TR};
   const uint32_t n = uint32_t(a.n_out);
-  const Operand cols{a.b + (uint64_t(where.expert) * n + col) * a.b_stride,
-                     a.b_stride, n - col < kTile ? n - col : kTile};
-  const uint32_t first = (threadIdx.x >> 7) * (kTile / 2) + (lane & 15);
-  const auto row_scale = [&](int f, uint32_t kb) -> int {
-    const uint32_t r = first + 16 * f;
-    const uint32_t p = where.first + (r < rows.rows ? r : rows.rows - 1);
-    return a.a_scales[p * a.a_scale_stride + kb];
-  };
-  const uint8_t *b_scale =
-      a.b_scales +
-      (uint64_t(where.expert) * ((n + 127) / 128) + col / 128) * a.b_scale_stride;
-  const auto col_scale = [&](int, uint32_t kb) -> int { return b_scale[kb]; };
-  f32x4 acc[kTile / 32][kTile / 32] = {};
-  multiply<T::kBytes == 4, kTile, kTile>(rows, cols, uint32_t(a.depth / 128),
-                                         lds, row_scale, col_scale, acc);
-  store_tile<kTile, kTile, T>(acc, a.out, a.out_stride, where.first, rows.rows,
-                              col, n, whole);
+  const Operand cols{
+      a.b + (uint64_t(where.expert) * n + col) * a.b_stride, a.b_stride,
+      a.b_scales + (uint64_t(where.expert) * ((n + 127) / 128) + col / 128) *
+                       a.b_scale_stride,
+      a.b_scale_stride, n - col < S::TC ? n - col : S::TC};
+  f32x4 acc[S::FR][S::FC] = {};
+  multiply<T::kBytes == 4, true, S>(rows, cols, 0, uint32_t(a.depth / 128), lds,
+                                    acc);
+  store_tile<S, T>(acc, a.out, a.out_stride, where.first, rows.rows, col, n,
+                   whole);
 }
 
 // Where an expert's columns start and how many there are, in blocks of 128
@@ -281,14 +328,14 @@ __device__ __forceinline__ void blocks_of_expert(const int32_t *offsets,
   blocks = hi > lo ? (hi - lo + 127) / 128 : 0;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256)
+template <typename S, typename T>
+__global__ void __launch_bounds__(S::kThreads)
     weight_grad_kernel(WeightGradArgs a, uint32_t row_tiles, uint32_t col_tiles,
                        bool whole) {
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * kTile * 128];
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[S::kLds];
   const uint32_t lane = threadIdx.x & 63;
-  const uint32_t col = (blockIdx.x % col_tiles) * kTile;
-  const uint32_t row = (blockIdx.x / col_tiles % row_tiles) * kTile;
+  const uint32_t col = (blockIdx.x % col_tiles) * S::TC;
+  const uint32_t row = (blockIdx.x / col_tiles % row_tiles) * S::TR;
   const uint32_t expert = blockIdx.x / col_tiles / row_tiles;
   uint32_t start, blocks;
   blocks_of_expert(a.offsets, expert, lane, start, blocks);
@@ -297,27 +344,16 @@ __global__ void __launch_bounds__(256)
   if (blocks > most - start) blocks = most - start;
   const uint32_t n = uint32_t(a.n_out), c = uint32_t(a.n_cols);
   const Operand rows{a.dy_t + row * a.length + uint64_t(start) * 128, a.length,
-                     n - row < kTile ? n - row : kTile};
+                     a.dy_scales + row * a.dy_scale_stride + (start & ~3u),
+                     a.dy_scale_stride, n - row < S::TR ? n - row : S::TR};
   const Operand cols{a.x_t + col * a.length + uint64_t(start) * 128, a.length,
-                     c - col < kTile ? c - col : kTile};
-  const uint32_t row0 = (threadIdx.x >> 7) * (kTile / 2) + (lane & 15);
-  const uint32_t col0 = ((threadIdx.x >> 6) & 1) * (kTile / 2) + (lane & 15);
-  const auto row_scale = [&](int f, uint32_t kb) -> int {
-    const uint32_t r = row0 + 16 * f;
-    return a.dy_scales[(row + (r < rows.rows ? r : rows.rows - 1)) *
-                           a.dy_scale_stride + start + kb];
-  };
-  const auto col_scale = [&](int g, uint32_t kb) -> int {
-    const uint32_t r = col0 + 16 * g;
-    return a.x_scales[(col + (r < cols.rows ? r : cols.rows - 1)) *
-                          a.x_scale_stride + start + kb];
-  };
-  f32x4 acc[kTile / 32][kTile / 32] = {};
+                     a.x_scales + col * a.x_scale_stride + (start & ~3u),
+                     a.x_scale_stride, c - col < S::TC ? c - col : S::TC};
+  f32x4 acc[S::FR][S::FC] = {};
   if (blocks > 0)
-    multiply<T::kBytes == 4, kTile, kTile>(rows, cols, blocks, lds, row_scale,
-                                           col_scale, acc);
-  store_tile<kTile, kTile, T>(acc, a.d_w, c, uint64_t(expert) * n + row,
-                              rows.rows, col, c, whole);
+    multiply<T::kBytes == 4, false, S>(rows, cols, start & 3, blocks, lds, acc);
+  store_tile<S, T>(acc, a.d_w, c, uint64_t(expert) * n + row, rows.rows, col, c,
+                   whole);
 }
 
 // Whether four consecutive results at columns that are multiples of 4 may be
@@ -327,33 +363,42 @@ bool aligned_fours(const void *out, uint64_t stride, uint32_t bytes) {
          (reinterpret_cast<uintptr_t>(out) & (4 * bytes - 1)) == 0;
 }
 
-template <typename T>
-hipError_t matmul_typed(const MatmulArgs &a, uint32_t row_tiles,
-                        uint32_t col_tiles, hipStream_t s) {
-  expert_matmul_kernel<T><<<dim3(row_tiles * col_tiles), dim3(256), 0, s>>>(
-      a, col_tiles, aligned_fours(a.out, a.out_stride, T::kBytes));
+template <typename S, typename T>
+hipError_t matmul_shaped(const MatmulArgs &a, hipStream_t s) {
+  const uint64_t some =
+      !a.offsets ? 1 : a.n_rows < a.n_experts ? a.n_rows : a.n_experts;
+  const uint32_t rt = uint32_t((a.n_rows + (S::TR - 1) * some) / S::TR);
+  const uint32_t ct = uint32_t((a.n_out + S::TC - 1) / S::TC);
+  expert_matmul_kernel<S, T><<<dim3(rt * ct), dim3(S::kThreads), 0, s>>>(
+      a, ct, aligned_fours(a.out, a.out_stride, T::kBytes));
   return hipGetLastError();
 }
 
 template <typename T>
+hipError_t matmul_typed(const MatmulArgs &a, hipStream_t s) {
+#ifndef SHAPE
+#define SHAPE Shape<256, 256, 2, 4>
+#endif
+  return matmul_shaped<SHAPE, T>(a, s);
+}
+
+template <typename T>
 hipError_t grad_typed(const WeightGradArgs &a, hipStream_t s) {
-  const uint32_t rt = uint32_t((a.n_out + kTile - 1) / kTile);
-  const uint32_t ct = uint32_t((a.n_cols + kTile - 1) / kTile);
-  weight_grad_kernel<T><<<dim3(a.n_experts * rt * ct), dim3(256), 0, s>>>(
-      a, rt, ct, aligned_fours(a.d_w, a.n_cols, T::kBytes));
+  using S = Shape<128, 128, 2, 2>;
+  const uint32_t rt = uint32_t((a.n_out + S::TR - 1) / S::TR);
+  const uint32_t ct = uint32_t((a.n_cols + S::TC - 1) / S::TC);
+  weight_grad_kernel<S, T>
+      <<<dim3(a.n_experts * rt * ct), dim3(S::kThreads), 0, s>>>(
+          a, rt, ct, aligned_fours(a.d_w, a.n_cols, T::kBytes));
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_expert_matmul(const MatmulArgs &a, hipStream_t s) {
-  const uint64_t some =
-      !a.offsets ? 1 : a.n_rows < a.n_experts ? a.n_rows : a.n_experts;
-  const uint32_t rt = uint32_t((a.n_rows + (kTile - 1) * some) / kTile);
-  const uint32_t ct = uint32_t((a.n_out + kTile - 1) / kTile);
-  return a.out_dtype == CIERA_DT_BF16   ? matmul_typed<Bf16>(a, rt, ct, s)
-         : a.out_dtype == CIERA_DT_FP16 ? matmul_typed<Fp16>(a, rt, ct, s)
-                                        : matmul_typed<Fp32>(a, rt, ct, s);
+  return a.out_dtype == CIERA_DT_BF16   ? matmul_typed<Bf16>(a, s)
+         : a.out_dtype == CIERA_DT_FP16 ? matmul_typed<Fp16>(a, s)
+                                        : matmul_typed<Fp32>(a, s);
 }
 
 hipError_t launch_weight_grad(const WeightGradArgs &a, hipStream_t s) {
