@@ -19,6 +19,8 @@
 // gradient), the "columns" operand its contiguous dimension (outputs n; inputs c).
 // The columns operand is the instruction's first: a lane's four results are
 // then consecutive in memory.
+#include <type_traits>
+
 #include "ciera_expert.h"
 #include "ciera_expert_dev.h"
 
@@ -69,23 +71,29 @@ __device__ __forceinline__ i32x8 fragment(const uint8_t *tile, uint32_t row,
 struct Wide {
   bf16x8 k[4];
 };
-__device__ __forceinline__ Wide widen(const i32x8 &f, int scale_byte) {
-  const float scale = __uint_as_float(uint32_t(scale_byte) << 23);
+__device__ __forceinline__ bf16x8 widen_piece(const i32x8 &f, uint32_t scale_byte,
+                                              int k) {
+  const float scale = __uint_as_float((scale_byte & 0xFF) << 23);
+  bf16x8 r;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(
+        uint32_t(f[2 * k + h]), scale, false);
+    const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(
+        uint32_t(f[2 * k + h]), scale, true);
+    r[4 * h] = lo[0];
+    r[4 * h + 1] = lo[1];
+    r[4 * h + 2] = hi[0];
+    r[4 * h + 3] = hi[1];
+  }
+  // stays where it is asked for: kept early it would take registers for long
+  asm volatile("" : "+v"(r));
+  return r;
+}
+__device__ __forceinline__ Wide widen(const i32x8 &f, uint32_t scale_byte) {
   Wide r;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(
-          uint32_t(f[2 * k + h]), scale, false);
-      const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(
-          uint32_t(f[2 * k + h]), scale, true);
-      r.k[k][4 * h] = lo[0];
-      r.k[k][4 * h + 1] = lo[1];
-      r.k[k][4 * h + 2] = hi[0];
-      r.k[k][4 * h + 3] = hi[1];
-    }
-  }
+  for (int k = 0; k < 4; ++k) r.k[k] = widen_piece(f, scale_byte, k);
   return r;
 }
 
@@ -226,10 +234,10 @@ __device__ __forceinline__ void multiply(const Operand &rows,
       Wide fr[FR];
 #pragma unroll
       for (int f = 0; f < FR; ++f)
-        fr[f] = widen(fragment(tr, row0 + 16 * f, quarter), sr[f]);
+        fr[f] = widen(fragment(tr, row0 + 16 * f, quarter), uint32_t(sr[f]));
 #pragma unroll
       for (int g = 0; g < FC; ++g) {
-        const Wide fc = widen(fragment(tc, col0 + 16 * g, quarter), sc[g]);
+        const Wide fc = widen(fragment(tc, col0 + 16 * g, quarter), uint32_t(sc[g]));
 #pragma unroll
         for (int k = 0; k < 4; ++k)
 #pragma unroll
@@ -308,6 +316,577 @@ __global__ void __launch_bounds__(S::kThreads)
                    whole);
 }
 
+// ---------------------------------------------------- streaming products ----
+// Results in 16 bits of many rows. A workgroup of four waves, one a SIMD, goes
+// through 256 x 256 tiles of the result without a pause between them; a wave
+// has 128 x 128 of a tile, in four quadrants of 4 x 4 fragments.
+//
+// What bounds it is the way from LDS: a block of a tile costs 64 KB written and 2
+// x 64 KB read there, against 2048 cycles of matrix instructions a SIMD (8 waves
+// of 128 x 64 read 192 KB). One wave a SIMD has to hide all latency itself:
+//   quadrant  (0,0)      (0,1)      | barrier |  (1,1)          (1,0)
+//   LDS reads  C1         R1        |         |  R0 of the next  C0 of the next
+//   loads                           | block two ahead, into the stage that is free
+// Rn and Cn are halves of the rows' and columns' fragments; each is read while the
+// quadrant before it is multiplied. One barrier a block, behind the last read of
+// its stage and the arrival of the next one. The results of a tile are stored
+// while the next tile's first block is multiplied, a quadrant ahead of the
+// instructions that overwrite it.
+struct Stream {
+  static constexpr int TR = 256, TC = 256;
+  static constexpr int kStage = (TR + TC) * 128;
+  static constexpr int kScales = (TR + TC) * 4;
+  // loads of a wave behind the last that is waited for, and stores of a quadrant
+  static constexpr int kBehind = 18, kStores = 8;
+};
+
+// Columns of a fragment. Row p = 4 u + i of fragment g is column 32 (g / 2) + 8 u
+// + 4 (g % 2) + i, so that a lane's results of two fragments are eight
+// neighbours: one 16-byte store. Chunk c of a column lies in LDS at c ^ col_key: the
+// 16 of a fragment then cover all banks.
+__device__ __forceinline__ constexpr uint32_t col_of(uint32_t p, uint32_t g) {
+  return 32 * (g >> 1) + 8 * (p >> 2) + 4 * (g & 1) + (p & 3);
+}
+__device__ __forceinline__ constexpr uint32_t col_key(uint32_t row) {
+  return ((row >> 1) & 1) | ((row >> 3) & 3) << 1;
+}
+
+// Raw 32-bit buffer: reads past `bytes` give 0, writes there are dropped. Its
+// words are the same in all lanes, which the compiler is told here: else it loops
+// over the lanes' values.
+__device__ __forceinline__ u32x4 resource(const void *p, uint32_t bytes) {
+  const uint64_t at = reinterpret_cast<uint64_t>(p);
+  return u32x4{uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(at))),
+               uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(at >> 32))),
+               uint32_t(__builtin_amdgcn_readfirstlane(bytes)), 0x00020000u};
+}
+// 16 or 4 bytes a lane from a buffer into LDS from byte to + TO on. Written as
+// assembly because the compiler waits for such loads before the next read of LDS,
+// whatever the addresses; here they are waited for at the barrier in front of the
+// reads. The lane's offset is lane_at + rows_at, added here so that neither takes a
+// register between the loads.
+template <uint32_t TO>
+__device__ __forceinline__ void buffer_to_lds16(u32x4 resource, uint32_t to,
+                                                uint32_t lane_at,
+                                                uint32_t rows_at,
+                                                uint32_t wave_at) {
+  uint32_t at;
+  asm volatile(
+      "s_add_u32 m0, %1, %6\n\tv_add_u32 %0, %3, %2\n\t"
+      "buffer_load_dwordx4 %0, %4, %5 offen lds"
+      : "=&v"(at)
+      : "s"(to), "v"(lane_at), "s"(rows_at), "s"(resource), "s"(wave_at),
+        "i"(TO)
+      : "scc");
+}
+template <uint32_t TO>
+__device__ __forceinline__ void buffer_to_lds4(u32x4 resource, uint32_t to,
+                                               uint32_t lane_at,
+                                               uint32_t wave_at) {
+  asm volatile(
+      "s_add_u32 m0, %0, %4\n\ts_nop 0\n\t"
+      "buffer_load_dword %1, %2, %3 offen lds"
+      :: "s"(to), "v"(lane_at), "s"(resource), "s"(wave_at), "i"(TO)
+      : "scc");
+}
+
+// Two results in 16 bits, rounded to nearest even.
+template <typename T>
+__device__ __forceinline__ uint32_t pack_pair(float a, float b) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+  const f32x2 v = {a, b};
+  if constexpr (std::is_same_v<T, Bf16>)
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+  else
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
+}
+
+// A tile of a result, everything the same for the whole workgroup.
+struct Job {
+  uint32_t expert;
+  uint32_t row, rows;  // first row (of all rows, or of the expert's result); 0 rows:
+                       // there is no tile
+  uint32_t col;
+  uint32_t start;  // block 0's place in the operands' rows
+  uint32_t real;   // blocks that there are; up to `steps` zeros are multiplied
+  uint32_t steps;  // even, at least 4
+};
+__device__ __forceinline__ uint32_t padded_steps(uint32_t real) {
+  return real < 4 ? 4u : (real + 1) & ~1u;
+}
+
+// The experts' sums in LDS: tiles (products) or blocks of 128 rows (gradients) in
+// front of each, and their rows.
+struct Sums {
+  uint32_t before[CIERA_MAX_EXPERTS + 1];
+  uint32_t first[CIERA_MAX_EXPERTS], last[CIERA_MAX_EXPERTS];
+};
+// By one wave.
+__device__ __forceinline__ void sum_experts(Sums &s, const int32_t *offsets,
+                                            uint32_t n_experts, uint32_t n_rows,
+                                            uint32_t log2_unit, uint32_t lane) {
+  uint32_t before = 0;
+  for (uint32_t from = 0; from < n_experts; from += 64) {
+    const uint32_t e = from + lane;
+    uint32_t lo = 0, hi = 0;
+    if (e < n_experts) {
+      lo = offsets ? offset_of(offsets, e, n_rows) : 0;
+      hi = offsets ? offset_of(offsets, e + 1, n_rows) : n_rows;
+      if (hi < lo) hi = lo;
+    }
+    uint32_t total;
+    const uint32_t start =
+        before +
+        wave_prefix((hi - lo + (1u << log2_unit) - 1) >> log2_unit, lane, total);
+    before += total;
+    if (e < n_experts) {
+      s.before[e] = start;
+      s.first[e] = lo;
+      s.last[e] = hi;
+      if (e == n_experts - 1) s.before[n_experts] = before;
+    }
+  }
+}
+// in all lanes, for the compiler
+__device__ __forceinline__ uint32_t same(uint32_t x) {
+  return __builtin_amdgcn_readfirstlane(x);
+}
+
+// What a stream multiplies: the order of its tiles and where their operands are.
+// Tiles in an order that the XCDs' caches like: the 32 workgroups of an XCD take 4
+// x 8 neighbours at a time (2 x 16: 896 us against 880 for 65,536 rows x 7168 x
+// 2048; workgroups in order: 903).
+struct ProductStream {
+  MatmulArgs a;
+  uint32_t row_tiles, col_tiles;
+  static constexpr bool kColBlocks = true;  // a scale for 128 of the columns
+  __device__ __forceinline__ uint32_t n_cols() const { return uint32_t(a.n_out); }
+  __device__ __forceinline__ void prepare(Sums &s, uint32_t lane) const {
+    sum_experts(s, a.offsets, a.n_experts, uint32_t(a.n_rows), 8, lane);
+  }
+  __device__ __forceinline__ Job job(const Sums &s, uint32_t t,
+                                     uint32_t lane) const {
+    Job j{0, 0, 0, 0, 0, 0, 4};
+    const uint32_t g = t / (4 * col_tiles), in = t % (4 * col_tiles);
+    const uint32_t tile = 4 * g + (in & 3);
+    if (tile >= row_tiles || tile >= same(s.before[a.n_experts])) return j;
+    uint32_t e = 0;  // experts that start at or before the tile
+    for (uint32_t from = 0; from < a.n_experts; from += 64)
+      e += __popcll(__ballot(from + lane < a.n_experts &&
+                             s.before[from + lane] <= tile));
+    j.expert = same(e - 1);
+    j.row = same(s.first[j.expert] + (tile - s.before[j.expert]) * Stream::TR);
+    const uint32_t held = same(s.last[j.expert]) - j.row;
+    j.rows = held < Stream::TR ? held : Stream::TR;
+    j.col = (in >> 2) * Stream::TC;
+    j.real = uint32_t(a.depth / 128);
+    j.steps = padded_steps(j.real);
+    return j;
+  }
+  __device__ __forceinline__ uint32_t row_stride() const { return uint32_t(a.a_stride); }
+  __device__ __forceinline__ uint32_t col_stride() const { return uint32_t(a.b_stride); }
+  __device__ __forceinline__ uint32_t row_scale_stride() const {
+    return uint32_t(a.a_scale_stride);
+  }
+  __device__ __forceinline__ uint32_t col_scale_stride() const {
+    return uint32_t(a.b_scale_stride);
+  }
+  __device__ __forceinline__ const uint8_t *rows(const Job &j) const {
+    return a.a + uint64_t(j.row) * a.a_stride;
+  }
+  __device__ __forceinline__ const uint8_t *cols(const Job &j) const {
+    return a.b + (uint64_t(j.expert) * a.n_out + j.col) * a.b_stride;
+  }
+  __device__ __forceinline__ const uint8_t *row_scales(const Job &j) const {
+    return a.a_scales + uint64_t(j.row) * a.a_scale_stride;
+  }
+  __device__ __forceinline__ const uint8_t *col_scales(const Job &j) const {
+    return a.b_scales + (uint64_t(j.expert) * ((a.n_out + 127) / 128) +
+                         j.col / 128) * a.b_scale_stride;
+  }
+  __device__ __forceinline__ uint64_t out_stride() const { return a.out_stride; }
+  __device__ __forceinline__ void *out() const { return a.out; }
+  __device__ __forceinline__ uint64_t out_row(const Job &j) const { return j.row; }
+};
+
+struct GradStream {
+  WeightGradArgs a;
+  uint32_t row_tiles, col_tiles;
+  uint32_t group;  // row tiles that are taken together; divides row_tiles
+  static constexpr bool kColBlocks = false;
+  __device__ __forceinline__ uint32_t n_cols() const { return uint32_t(a.n_cols); }
+  __device__ __forceinline__ void prepare(Sums &s, uint32_t lane) const {
+    sum_experts(s, a.offsets, a.n_experts, ~0u, 7, lane);
+  }
+  __device__ __forceinline__ Job job(const Sums &s, uint32_t t, uint32_t) const {
+    Job j{0, 0, 0, 0, 0, 0, 4};
+    const uint32_t whole = row_tiles * col_tiles;
+    j.expert = t / whole;
+    if (j.expert >= a.n_experts) return j;
+    const uint32_t in_expert = t % whole, g = in_expert / (group * col_tiles);
+    const uint32_t in = in_expert % (group * col_tiles);
+    j.row = (group * g + in % group) * Stream::TR;
+    const uint32_t held = uint32_t(a.n_out) - j.row;
+    j.rows = held < Stream::TR ? held : Stream::TR;
+    j.col = in / group * Stream::TC;
+    const uint32_t most = uint32_t(a.length / 128);
+    const uint32_t start = same(s.before[j.expert]);
+    const uint32_t end = same(s.before[j.expert + 1]);
+    j.start = start < most ? start : most;
+    j.real = (end < most ? end : most) - j.start;
+    j.steps = padded_steps(j.real);
+    return j;
+  }
+  __device__ __forceinline__ uint32_t row_stride() const { return uint32_t(a.length); }
+  __device__ __forceinline__ uint32_t col_stride() const { return uint32_t(a.length); }
+  __device__ __forceinline__ uint32_t row_scale_stride() const {
+    return uint32_t(a.dy_scale_stride);
+  }
+  __device__ __forceinline__ uint32_t col_scale_stride() const {
+    return uint32_t(a.x_scale_stride);
+  }
+  __device__ __forceinline__ const uint8_t *rows(const Job &j) const {
+    return a.dy_t + uint64_t(j.row) * a.length + uint64_t(j.start) * 128;
+  }
+  __device__ __forceinline__ const uint8_t *cols(const Job &j) const {
+    return a.x_t + uint64_t(j.col) * a.length + uint64_t(j.start) * 128;
+  }
+  // the dword that holds block 0's
+  __device__ __forceinline__ const uint8_t *row_scales(const Job &j) const {
+    return a.dy_scales + uint64_t(j.row) * a.dy_scale_stride + (j.start & ~3u);
+  }
+  __device__ __forceinline__ const uint8_t *col_scales(const Job &j) const {
+    return a.x_scales + uint64_t(j.col) * a.x_scale_stride + (j.start & ~3u);
+  }
+  __device__ __forceinline__ uint64_t out_stride() const { return a.n_cols; }
+  __device__ __forceinline__ void *out() const { return a.d_w; }
+  __device__ __forceinline__ uint64_t out_row(const Job &j) const {
+    return uint64_t(j.expert) * a.n_out + j.row;
+  }
+};
+
+template <typename T, typename P>
+__global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
+  __shared__ __attribute__((aligned(1024)))
+  uint8_t lds[2 * (Stream::kStage + Stream::kScales)];
+  __shared__ Sums sums;
+  const uint32_t lane = threadIdx.x & 63;
+  const uint32_t wave = same(threadIdx.x >> 6);
+  if (wave == 0) what.prepare(sums, lane);
+  __syncthreads();
+  // the XCD's share of the grid's tiles, and the workgroup's place in it
+  uint32_t tile = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
+  Job job = what.job(sums, tile, lane);
+  if (job.rows == 0) return;
+
+  // ---- loading ----
+  // A wave loads 32 rows of each half of both operands, as 4 instructions of 8.
+  const uint32_t row_stride = what.row_stride(), col_stride = what.col_stride();
+  const uint32_t wave_row = (wave >> 1) * 128 + (wave & 1) * 32;
+  uint32_t row_at[2], col_at[4];
+#pragma unroll
+  for (uint32_t i = 0; i < 4; ++i) {
+    const uint32_t r = wave_row + i * 8 + (lane >> 3);
+    if (i < 2)
+      row_at[i] = r * row_stride + (((lane & 7) ^ ((r >> 1) & 7)) << 4);
+    col_at[i] = r * col_stride + (((lane & 7) ^ col_key(r)) << 4);
+  }
+  // Scales: place 8 p + f of a half of 128 holds the dword of the row that lane p
+  // has in fragment f, so that a lane's eight are two 16-byte reads.
+  const uint32_t place = (wave & 1) * 64 + lane;
+  const uint32_t row_scale_at =
+      ((wave >> 1) * 128 + 16 * (place & 7) + (place >> 3)) *
+      what.row_scale_stride();
+  const uint32_t col_scale_at =
+      (P::kColBlocks ? wave >> 1
+                     : (wave >> 1) * 128 + col_of(place >> 3, place & 7)) *
+      what.col_scale_stride();
+  u32x4 rr, rc, rrs, rcs;
+  uint32_t bytes_r, bytes_c, bytes_rs, bytes_cs, real, load_phase;
+  // the tile that is loaded from now on; without one nothing is read
+  const auto aim = [&](const Job &j) {
+    const uint32_t cols =
+        what.n_cols() - j.col < Stream::TC ? what.n_cols() - j.col : Stream::TC;
+    rr = resource(what.rows(j), 0);
+    rc = resource(what.cols(j), 0);
+    rrs = resource(what.row_scales(j), 0);
+    rcs = resource(what.col_scales(j), 0);
+    real = j.rows != 0 ? j.real : 0;
+    load_phase = j.start & 3;
+    bytes_r = same((j.rows - 1) * row_stride + real * 128);
+    bytes_c = same((cols - 1) * col_stride + real * 128);
+    bytes_rs = same(j.rows * what.row_scale_stride());
+    bytes_cs = same((P::kColBlocks ? (cols + 127) / 128 : cols) *
+                    what.col_scale_stride());
+  };
+  // block kb of it: one that is not there is zeros
+  const auto point = [&](uint32_t kb) {
+    rr[2] = kb < real ? bytes_r : 0;
+    rc[2] = kb < real ? bytes_c : 0;
+    rrs[2] = kb < real ? bytes_rs : 0;
+    rcs[2] = kb < real ? bytes_cs : 0;
+  };
+  const uint32_t lds0 = uint32_t(reinterpret_cast<uintptr_t>(
+      (__attribute__((address_space(3))) uint8_t *)lds));
+  const uint32_t lds_rows = lds0 + wave_row * 128;
+  const uint32_t lds_cols = lds0 + (Stream::TR + wave_row) * 128;
+  const uint32_t lds_row_scales = lds0 + 2 * Stream::kStage + wave * 256;
+  const uint32_t lds_col_scales = lds_row_scales + Stream::TR * 4;
+  // Instruction i < 4 of half h. A row's place is in the lane's offset: rows that
+  // are not there fail the range check and are not read.
+  const auto load_row = [&](auto h, auto i, auto stage, uint32_t kb) {
+    constexpr uint32_t n = decltype(i)::value, half = 64 * decltype(h)::value;
+    buffer_to_lds16<decltype(stage)::value * Stream::kStage +
+                    (half + 8 * n) * 128>(rr, lds_rows, row_at[n & 1],
+                                          (half + (n & 2) * 8) * row_stride,
+                                          kb * 128);
+  };
+  const auto load_col = [&](auto h, auto i, auto stage, uint32_t kb) {
+    constexpr uint32_t n = decltype(i)::value;
+    constexpr uint32_t half = 64 * decltype(h)::value;
+    buffer_to_lds16<decltype(stage)::value * Stream::kStage + (half + 8 * n) * 128>(
+        rc, lds_cols, col_at[n], half * col_stride, kb * 128);
+  };
+  const auto load_scales = [&](auto stage, uint32_t kb) {
+    constexpr uint32_t at = decltype(stage)::value * Stream::kScales;
+    const uint32_t dword = (load_phase + kb) & ~3u;
+    buffer_to_lds4<at>(rrs, lds_row_scales, row_scale_at, dword);
+    buffer_to_lds4<at>(rcs, lds_col_scales, col_scale_at, dword);
+  };
+
+  // ---- multiplying ----
+  f32x4 acc[8][8];  // [rows' fragment][columns' fragment]
+  // The columns' halves change places from block to block: C0 of the next one goes
+  // where this one's C1 was.
+  i32x8 r0[4], r1[4], cs[2][4];
+  uint32_t sr[2][8], sc[2][8];
+  const uint32_t row0 = (wave >> 1) * 128, col0 = (wave & 1) * 128;
+  const uint32_t p = lane & 15, quarter = lane >> 4;
+  const uint32_t row_lo = place_of(row0 + p, quarter);
+  const uint32_t row_hi = place_of(row0 + p, quarter + 4);
+  const uint32_t col_row = col0 + col_of(p, 0);
+  const uint32_t col_lo = Stream::TR * 128 + col_row * 128 +
+                          ((quarter ^ col_key(col_row)) << 4);
+  const uint32_t col_hi = Stream::TR * 128 + col_row * 128 +
+                          (((quarter + 4) ^ col_key(col_row)) << 4);
+  const auto joined = [&](uint32_t lo_at, uint32_t hi_at) -> i32x8 {
+    const i32x4 lo = *reinterpret_cast<const i32x4 *>(lds + lo_at);
+    const i32x4 hi = *reinterpret_cast<const i32x4 *>(lds + hi_at);
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  const auto read_row = [&](uint32_t f, uint32_t stage) -> i32x8 {
+    const uint32_t at = stage * Stream::kStage + f * 2048;
+    return joined(row_lo + at, row_hi + at);
+  };
+  const auto read_col = [&](uint32_t g, uint32_t stage) -> i32x8 {
+    const uint32_t at = stage * Stream::kStage + col_of(0, g) * 128;
+    return joined(col_lo + at, col_hi + at);
+  };
+  // dwords of scales: rows' fragments 0 ... 7, then columns'
+  const auto read_scales = [&](u32x4(&to)[4], uint32_t stage) {
+    const uint8_t *s = lds + 2 * Stream::kStage + stage * Stream::kScales;
+    const uint8_t *r = s + (row0 + 8 * p) * 4;
+    const uint8_t *c = s + (Stream::TR + col0 + 8 * p) * 4;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      to[h] = *reinterpret_cast<const u32x4 *>(r + 16 * h);
+      to[2 + h] = *reinterpret_cast<const u32x4 *>(c + 16 * h);
+    }
+  };
+  // fragment k's of a block at place `at` counted from the first dword's
+  const auto use_scales = [&](int which, const u32x4(&from)[4], uint32_t at,
+                              int k) {
+    sr[which][k] = from[k / 4][k % 4] >> (8 * (at & 3));
+    sc[which][k] = from[2 + k / 4][k % 4] >> (8 * (at & 3));
+  };
+  // fragment pairs [from, from + count) of a quadrant's 16
+  const auto multiply = [&](auto first, auto stage, int hr, int hc,
+                            const i32x8(&r)[4], const i32x8(&c)[4], int from,
+                            int count) {
+    constexpr int kNow = decltype(stage)::value;
+#pragma unroll
+    for (int i = from; i < from + count; ++i) {
+      const int g = i / 4, f = i % 4;
+      f32x4 &d = acc[4 * hr + f][4 * hc + g];
+      const f32x4 zero = {0, 0, 0, 0};
+      d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+          c[g], r[f], decltype(first)::value ? zero : d, 0, 0, 0,
+          int(sc[kNow][4 * hc + g]), 0, int(sr[kNow][4 * hr + f]));
+      // keeps its place among the loads, which are volatile as well
+      asm volatile("" : "+a"(d));
+    }
+  };
+  // the tile whose results are still in registers
+  Job held{0, 0, 0, 0, 0, 0, 4};
+  const uint32_t out_stride = uint32_t(what.out_stride()) * T::kBytes;
+  const uint32_t out_at =
+      (row0 + p) * out_stride + (col0 + 8 * quarter) * T::kBytes;
+  // piece i < 8 of a quadrant: a rows' fragment, eight columns a lane
+  const auto store = [&](int hr, int hc, int i) {
+    const int f = i / 2, g = 2 * (i % 2);
+    uint32_t stride = out_stride;
+    asm volatile("" : "+s"(stride));  // what follows from it is not kept
+    const u32x4 words =
+        resource(static_cast<uint8_t *>(what.out()) +
+                     (what.out_row(held) * what.out_stride() + held.col) *
+                         T::kBytes,
+                 Stream::TR * out_stride);
+    const auto out = __builtin_amdgcn_make_buffer_rsrc(
+        reinterpret_cast<void *>(uint64_t(words[1]) << 32 | words[0]), 0,
+        words[2], words[3]);
+    u32x4 w;
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      const f32x4 v = acc[4 * hr + f][4 * hc + g + h / 2];
+      w[h] = pack_pair<T>(v[2 * (h % 2)], v[2 * (h % 2) + 1]);
+    }
+    // dropped by the range check where there is no such row or column
+    const bool there =
+        int(p) < int(held.rows - row0) - 64 * hr - 16 * f &&
+        int(8 * quarter) <
+            int(what.n_cols() - held.col - col0) - 64 * hc - 16 * g;
+    __builtin_amdgcn_raw_buffer_store_b128(
+        w, out, there ? out_at : ~0u,
+        (64 * hr + 16 * f) * stride + (64 * hc + 16 * g) * T::kBytes, 0);
+  };
+
+  // A block of the tile, in stage 0 or 1. It loads block load_kb of the tile that is
+  // aimed at, two blocks ahead. The order of the instructions is the order here: a
+  // read or load between every few matrix instructions, so that neither holds up the
+  // wave.
+  const auto in_order = [] { __builtin_amdgcn_sched_barrier(0); };
+  const auto each = [](auto body) {
+    body(std::integral_constant<uint32_t, 0>{});
+    body(std::integral_constant<uint32_t, 1>{});
+    body(std::integral_constant<uint32_t, 2>{});
+    body(std::integral_constant<uint32_t, 3>{});
+  };
+  constexpr std::integral_constant<uint32_t, 0> even{};  // stages, and halves
+  constexpr std::integral_constant<uint32_t, 1> odd{};
+  const auto block = [&](auto first, auto stage, uint32_t next_at,
+                         uint32_t load_kb) {
+    constexpr bool kFirst = decltype(first)::value;
+    constexpr uint32_t kNow = decltype(stage)::value, kNext = kNow ^ 1;
+    i32x8(&c0)[4] = cs[kNow];
+    i32x8(&c1)[4] = cs[kNext];
+    // a quarter of a quadrant of the last tile's results
+    const auto old = [&](int hr, int hc, int i) {
+      if constexpr (kFirst) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          store(hr, hc, 2 * i + k);
+          in_order();
+        }
+      }
+    };
+    point(load_kb);
+    each([&](auto i) { old(0, 0, i.value); });
+    in_order();
+    each([&](auto i) {
+      c1[i.value] = read_col(4 + i.value, kNow);
+      load_row(even, i, stage, load_kb);
+      multiply(first, stage, 0, 0, r0, c0, 4 * i.value, 2);
+      in_order();
+      load_col(even, i, stage, load_kb);
+      multiply(first, stage, 0, 0, r0, c0, 4 * i.value + 2, 2);
+      in_order();
+      old(0, 1, i.value);
+    });
+    load_scales(stage, load_kb);
+    each([&](auto i) {
+      r1[i.value] = read_row(4 + i.value, kNow);
+      multiply(first, stage, 0, 1, r0, c1, 2 * i.value, 2);
+      in_order();
+      old(1, 1, i.value);
+    });
+    multiply(first, stage, 0, 1, r0, c1, 8, 8);
+    in_order();
+    // The first half of the next block has arrived, and this wave has read the
+    // second half of this one. Behind those loads there are others, and a tile's
+    // stores.
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier"
+                 :: "i"(Stream::kBehind + (kFirst ? 3 * Stream::kStores : 0)) : "memory");
+    in_order();
+    u32x4 scales[4];
+    read_scales(scales, kNext);
+    each([&](auto i) {
+      r0[i.value] = read_row(i.value, kNext);
+      load_row(odd, i, stage, load_kb);
+      multiply(first, stage, 1, 1, r1, c1, 4 * i.value, 4);
+      in_order();
+      old(1, 0, i.value);
+    });
+    each([&](auto i) {
+      c1[i.value] = read_col(i.value, kNext);
+      load_col(odd, i, stage, load_kb);
+      multiply(first, stage, 1, 0, r1, c0, 2 * i.value, 2);
+      use_scales(kNext, scales, next_at, 2 * i.value);
+      use_scales(kNext, scales, next_at, 2 * i.value + 1);
+      in_order();
+    });
+    multiply(first, stage, 1, 0, r1, c0, 8, 8);
+    in_order();
+    // the same of the second half of the next block, and the first half of it
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier"
+                 :: "i"(Stream::kBehind + (kFirst ? 4 * Stream::kStores : 0)) : "memory");
+    in_order();
+  };
+
+  aim(job);
+  const auto load_block = [&](auto stage, uint32_t kb) {
+    point(kb);
+    each([&](auto i) {
+      load_row(even, i, stage, kb);
+      load_row(odd, i, stage, kb);
+      load_col(even, i, stage, kb);
+      load_col(odd, i, stage, kb);
+    });
+    load_scales(stage, kb);
+  };
+  load_block(even, 0);
+  load_block(odd, 1);
+  asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+  each([&](auto i) {
+    r0[i.value] = read_row(i.value, 0);
+    cs[0][i.value] = read_col(i.value, 0);
+  });
+  {
+    u32x4 scales[4];
+    read_scales(scales, 0);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) use_scales(0, scales, job.start, k);
+  }
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  do {
+    Job next{0, 0, 0, 0, 0, 0, 4};
+    block(std::true_type{}, even, job.start + 1, 2);
+    uint32_t load_kb = 3;
+    for (uint32_t kb = 1;; kb += 2) {
+      const bool last = kb + 1 == job.steps;
+      block(std::false_type{}, odd, last ? next.start : job.start + kb + 1,
+            load_kb++);
+      if (last) break;
+      if (kb + 1 == job.steps - 2) {
+        tile += gridDim.x;
+        next = what.job(sums, tile, lane);
+        aim(next);
+        load_kb = 0;
+      }
+      block(std::false_type{}, even, job.start + kb + 2, load_kb++);
+    }
+    held = job;
+    job = next;
+  } while (job.rows != 0);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    store(0, 0, i);
+    store(0, 1, i);
+    store(1, 1, i);
+    store(1, 0, i);
+  }
+}
+
 // Where an expert's columns start and how many there are, in blocks of 128
 // rows.
 __device__ __forceinline__ void blocks_of_expert(const int32_t *offsets,
@@ -374,23 +953,72 @@ hipError_t matmul_shaped(const MatmulArgs &a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <typename T>
-hipError_t matmul_typed(const MatmulArgs &a, hipStream_t s) {
-#ifndef SHAPE
-#define SHAPE Shape<256, 256, 2, 4>
-#endif
-  return matmul_shaped<SHAPE, T>(a, s);
+// What the streams' 32-bit offsets and 16-byte stores need.
+bool stream_fits(uint64_t row_stride, uint64_t col_stride,
+                 uint64_t row_scale_stride, uint64_t col_scale_stride,
+                 const void *out, uint64_t out_stride, uint64_t n_cols) {
+  constexpr uint64_t kMost = uint64_t(1) << 23;
+  return row_stride <= kMost && col_stride <= kMost &&
+         row_scale_stride <= kMost && col_scale_stride <= kMost &&
+         out_stride <= kMost / 4 && out_stride % 8 == 0 && n_cols % 8 == 0 &&
+         (reinterpret_cast<uintptr_t>(out) & 15) == 0;
+}
+constexpr uint32_t kStreamGroups = 256;  // one a CU
+
+// Tiles of 256 x 256 where there are enough for the CUs: four times the products
+// of 128 x 128 for twice the bytes.
+bool many_tiles(uint64_t rows, uint64_t cols) {
+  return ((rows + 255) / 256) * ((cols + 255) / 256) >= 256;
 }
 
 template <typename T>
-hipError_t grad_typed(const WeightGradArgs &a, hipStream_t s) {
-  using S = Shape<128, 128, 2, 2>;
+hipError_t matmul_typed(const MatmulArgs &a, hipStream_t s) {
+  if constexpr (T::kBytes == 2) {
+    if (a.depth >= 512 &&
+        stream_fits(a.a_stride, a.b_stride, a.a_scale_stride,
+                    a.b_scale_stride, a.out, a.out_stride, a.n_out)) {
+      const uint64_t some =
+          !a.offsets ? 1 : a.n_rows < a.n_experts ? a.n_rows : a.n_experts;
+      const ProductStream what{
+          a, uint32_t((a.n_rows + (Stream::TR - 1) * some) / Stream::TR),
+          uint32_t((a.n_out + Stream::TC - 1) / Stream::TC)};
+      stream_kernel<T><<<dim3(kStreamGroups), dim3(256), 0, s>>>(what);
+      return hipGetLastError();
+    }
+  }
+  return many_tiles(a.n_rows, a.n_out)
+             ? matmul_shaped<Shape<256, 256, 4, 2>, T>(a, s)
+             : matmul_shaped<Shape<128, 128, 2, 2>, T>(a, s);
+}
+
+template <typename S, typename T>
+hipError_t grad_shaped(const WeightGradArgs &a, hipStream_t s) {
   const uint32_t rt = uint32_t((a.n_out + S::TR - 1) / S::TR);
   const uint32_t ct = uint32_t((a.n_cols + S::TC - 1) / S::TC);
   weight_grad_kernel<S, T>
       <<<dim3(a.n_experts * rt * ct), dim3(S::kThreads), 0, s>>>(
           a, rt, ct, aligned_fours(a.d_w, a.n_cols, T::kBytes));
   return hipGetLastError();
+}
+
+template <typename T>
+hipError_t grad_typed(const WeightGradArgs &a, hipStream_t s) {
+  if constexpr (T::kBytes == 2) {
+    if (a.length > 0 &&
+        stream_fits(a.length, a.length, a.dy_scale_stride, a.x_scale_stride,
+                    a.d_w, a.n_cols, a.n_cols)) {
+      const uint32_t rt = uint32_t((a.n_out + Stream::TR - 1) / Stream::TR);
+      const uint32_t ct = uint32_t((a.n_cols + Stream::TC - 1) / Stream::TC);
+      const uint32_t group =
+          rt <= 8 ? rt : rt % 4 == 0 ? 4 : rt % 2 == 0 ? 2 : 1;
+      const GradStream what{a, rt, ct, group};
+      stream_kernel<T><<<dim3(kStreamGroups), dim3(256), 0, s>>>(what);
+      return hipGetLastError();
+    }
+  }
+  return many_tiles(a.n_out * a.n_experts, a.n_cols)
+             ? grad_shaped<Shape<256, 256, 4, 2>, T>(a, s)
+             : grad_shaped<Shape<128, 128, 2, 2>, T>(a, s);
 }
 
 }  // namespace

@@ -224,7 +224,12 @@ def whole_values(rows, cols, filled, seed, per_row=1):
     ([128, 0, 129, 1], 128, 640), ([0, 0], 130, 128),
     ([300, 5, 0, 127, 260], 257, 1024), ([3] * 70, 100, 256),
     ([0] * 100 + [200] + [0] * 30, 36, 512), ([1, 2, 3, 4, 0, 5, 1, 9], 511, 1920),
-    ([2000, 700, 33], 700, 512)])
+    ([2000, 700, 33], 700, 512),
+    # results of whole octets: even, odd and few blocks of the depth, tiles cut in
+    # rows and columns, experts without rows, several tiles a workgroup
+    ([300, 5, 0, 127, 260], 264, 1024), ([1], 8, 512), ([0, 0], 128, 640),
+    ([256, 255, 257], 256, 640), ([70, 0, 513], 1096, 896),
+    ([40] * 90, 1032, 512), ([0] * 100 + [200] + [0] * 30, 40, 2176)])
 def test_matmul(cl, dtype, counts, N, D):
     off = offsets_of(counts)
     E, held = len(counts), int(off[-1])
