@@ -19,6 +19,7 @@
 // gradient), the "columns" operand its contiguous dimension (outputs n; inputs c).
 // The columns operand is the instruction's first: a lane's four results are
 // then consecutive in memory.
+#include <cmath>
 #include <type_traits>
 
 #include "ciera_expert.h"
@@ -314,6 +315,129 @@ __global__ void __launch_bounds__(S::kThreads)
                                     acc);
   store_tile<S, T>(acc, a.out, a.out_stride, where.first, rows.rows, col, n,
                    whole);
+}
+
+// ------------------------------------------------------------- few rows ----
+// Experts with few rows each: what counts is to have the weights under way. They are
+// used once, so they go from memory into registers, 16 columns a wave, a batch of
+// blocks at a time and the next batch behind it; FR fragments of 16 rows come the
+// same way, out of the caches. Where columns alone make too few waves, SPLIT waves
+// share 16 columns, each with a part of the depth, and add up through LDS.
+template <typename T, int FR, int SPLIT>
+__global__ void __launch_bounds__(256)
+    few_rows_kernel(MatmulArgs a, uint32_t col_groups, bool whole) {
+  constexpr bool kExact = T::kBytes == 4;
+  constexpr uint32_t kGroups = 4 / SPLIT;  // of columns, a workgroup
+  constexpr uint32_t kRows = 16 * FR;
+  constexpr uint32_t kBatch = FR == 1 ? 4 : 2;  // blocks
+  __shared__ f32x4 parts[SPLIT > 1 ? 4 : 1][SPLIT > 1 ? FR : 1][64];
+  const uint32_t lane = threadIdx.x & 63;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t tile = blockIdx.x / col_groups;
+  const uint32_t col =
+      ((blockIdx.x % col_groups) * kGroups + wave / SPLIT) * 16;
+  ExpertTile where{0, tile * kRows, uint32_t(a.n_rows)};
+  if (a.offsets)
+    where = find_tile(a.offsets, a.n_experts, uint32_t(a.n_rows), tile,
+                      __builtin_ctz(kRows), lane);
+  if (where.expert == kNoExpert) return;
+  const uint32_t n = uint32_t(a.n_out), p = lane & 15, quarter = lane >> 4;
+  const uint32_t rows = where.end - where.first < kRows
+                            ? where.end - where.first : kRows;
+  const uint32_t blocks = uint32_t(a.depth / 128);
+  // parts of whole dwords of scales
+  const uint32_t part = ((blocks + SPLIT - 1) / SPLIT + 3) / 4 * 4;
+  const uint32_t from = wave % SPLIT * part;
+  const uint32_t to = from + part < blocks ? from + part : blocks;
+  f32x4 acc[FR] = {};
+  if (col < n && from < to) {
+    const uint32_t c = col + p < n ? col + p : n - 1;
+    const uint8_t *w = a.b + (uint64_t(where.expert) * n + c) * a.b_stride +
+                       quarter * 16;
+    const uint8_t *ws = a.b_scales +
+                        (uint64_t(where.expert) * ((n + 127) / 128) + col / 128) *
+                            a.b_scale_stride;
+    const uint8_t *x[FR], *xs[FR];
+#pragma unroll
+    for (int f = 0; f < FR; ++f) {
+      const uint32_t r = 16 * f + p;
+      const uint64_t row = where.first + (r < rows ? r : rows - 1);
+      x[f] = a.a + row * a.a_stride + quarter * 16;
+      xs[f] = a.a_scales + row * a.a_scale_stride;
+    }
+    struct Batch {
+      i32x4 w[kBatch][2], x[FR][kBatch][2];
+      uint32_t ws, xs[FR];
+    };
+    const auto load = [&](Batch &b, uint32_t kb) {
+#pragma unroll
+      for (uint32_t i = 0; i < kBatch; ++i) {
+        const uint64_t at = uint64_t(kb + i < to ? kb + i : to - 1) * 128;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          b.w[i][h] = __builtin_nontemporal_load(
+              reinterpret_cast<const i32x4 *>(w + at + 64 * h));
+#pragma unroll
+          for (int f = 0; f < FR; ++f)
+            b.x[f][i][h] = *reinterpret_cast<const i32x4 *>(x[f] + at + 64 * h);
+        }
+      }
+      b.ws = *reinterpret_cast<const uint32_t *>(ws + (kb & ~3u));
+#pragma unroll
+      for (int f = 0; f < FR; ++f)
+        b.xs[f] = *reinterpret_cast<const uint32_t *>(xs[f] + (kb & ~3u));
+    };
+    const auto joined = [](const i32x4(&h)[2]) -> i32x8 {
+      return __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    const auto use = [&](const Batch &b, uint32_t kb) {
+#pragma unroll
+      for (uint32_t i = 0; i < kBatch; ++i) {
+        if (kb + i >= to) break;
+        const uint32_t shift = 8 * ((kb + i) & 3);
+        if constexpr (kExact) {
+          const Wide ww = widen(joined(b.w[i]), b.ws >> shift);
+#pragma unroll
+          for (int f = 0; f < FR; ++f) {
+            const Wide wx = widen(joined(b.x[f][i]), b.xs[f] >> shift);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                  ww.k[k], wx.k[k], acc[f], 0, 0, 0);
+          }
+        } else {
+#pragma unroll
+          for (int f = 0; f < FR; ++f)
+            acc[f] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                joined(b.w[i]), joined(b.x[f][i]), acc[f], 0, 0, 0,
+                int(b.ws >> shift), 0, int(b.xs[f] >> shift));
+        }
+      }
+    };
+    Batch now, next;
+    load(now, from);
+    for (uint32_t kb = from; kb < to; kb += kBatch) {
+      if (kb + kBatch < to) load(next, kb + kBatch);
+      use(now, kb);
+      now = next;
+    }
+  }
+  if constexpr (SPLIT > 1) {
+#pragma unroll
+    for (int f = 0; f < FR; ++f) parts[wave][f][lane] = acc[f];
+    __syncthreads();
+    if (wave % SPLIT != 0) return;
+#pragma unroll
+    for (int k = 1; k < SPLIT; ++k)
+#pragma unroll
+      for (int f = 0; f < FR; ++f) acc[f] += parts[wave + k][f][lane];
+  }
+  const uint32_t c = col + 4 * quarter;
+#pragma unroll
+  for (int f = 0; f < FR; ++f)
+    if (16 * f + p < rows && c < n)
+      store_four<T>(a.out, (where.first + 16 * f + p) * a.out_stride + c, n - c,
+                    whole, acc[f]);
 }
 
 // ---------------------------------------------------- streaming products ----
@@ -971,16 +1095,67 @@ bool many_tiles(uint64_t rows, uint64_t cols) {
   return ((rows + 255) / 256) * ((cols + 255) / 256) >= 256;
 }
 
+template <typename T, int FR, int SPLIT>
+hipError_t few_split(const MatmulArgs &a, uint32_t tiles, hipStream_t s) {
+  const uint32_t groups = uint32_t((a.n_out + 64 / SPLIT - 1) / (64 / SPLIT));
+  few_rows_kernel<T, FR, SPLIT><<<dim3(tiles * groups), dim3(256), 0, s>>>(
+      a, groups, aligned_fours(a.out, a.out_stride, T::kBytes));
+  return hipGetLastError();
+}
+// As many parts of the depth as give every CU 16 waves, of four blocks or more.
+template <typename T, int FR>
+hipError_t few_rows(const MatmulArgs &a, uint64_t experts, hipStream_t s) {
+  const uint32_t tiles =
+      uint32_t((a.n_rows + (16 * FR - 1) * experts) / (16 * FR));
+  const uint64_t waves = tiles * ((a.n_out + 15) / 16);
+  if (waves >= 4096 || a.depth <= 512) return few_split<T, FR, 1>(a, tiles, s);
+  if (waves >= 2048 || a.depth <= 1024) return few_split<T, FR, 2>(a, tiles, s);
+  return few_split<T, FR, 4>(a, tiles, s);
+}
+
+// Fragments of rows for few_rows, or 0: tiles are faster. Times in us of few_rows with
+// 1 and 4 fragments / of 256 x 256 tiles, bf16:
+//   experts x N x depth    rows    1 fragment   4 fragments   tiles
+//   64 x 2048 x 1024        128        27            -           31
+//                           512        38           50           33
+//                          2048        85           71           35
+//   1 x 4096 x 7168          16        15           20           70
+//                            64        35           26           71
+//                           200       100           70           73
+// Tiles cost a round of the CUs for every 256 of them, 1.6 us a block of the depth.
+// few_rows reads the weights anew for every 16 or 64 rows of an expert, at 4 and 1.6 TB/s
+// with what else it does; an expert's last rows fill half of such a group. fp32 results
+// take tiles twice as long. With a row or two an expert the weights' own bytes are all.
+int few_fragments(const MatmulArgs &a, uint64_t experts, bool fp32) {
+  if (a.n_rows <= 2 * experts) return 1;
+  const auto groups = [&](uint64_t of) {
+    const uint64_t g = a.n_rows / of + experts / 2;
+    return double(g > experts ? g : experts);
+  };
+  const double weight = double(a.n_out) * double(a.depth);
+  const double rounds = std::ceil(
+      groups(256) * std::ceil(double(a.n_out) / 256) / kStreamGroups);
+  const double tiles =
+      6 + rounds * double(a.depth / 128) * (fp32 ? 3.2 : 1.6);
+  const double one = groups(16) * weight / 4.0e6;
+  const double four = groups(64) * weight / 1.6e6;
+  if (one <= four && one < tiles) return 1;
+  return four < tiles ? 4 : 0;
+}
+
 template <typename T>
 hipError_t matmul_typed(const MatmulArgs &a, hipStream_t s) {
+  const uint64_t experts =
+      !a.offsets ? 1 : a.n_rows < a.n_experts ? a.n_rows : a.n_experts;
+  const int few = few_fragments(a, experts, T::kBytes == 4);
+  if (few == 1) return few_rows<T, 1>(a, experts, s);
+  if (few == 4) return few_rows<T, 4>(a, experts, s);
   if constexpr (T::kBytes == 2) {
     if (a.depth >= 512 &&
         stream_fits(a.a_stride, a.b_stride, a.a_scale_stride,
                     a.b_scale_stride, a.out, a.out_stride, a.n_out)) {
-      const uint64_t some =
-          !a.offsets ? 1 : a.n_rows < a.n_experts ? a.n_rows : a.n_experts;
       const ProductStream what{
-          a, uint32_t((a.n_rows + (Stream::TR - 1) * some) / Stream::TR),
+          a, uint32_t((a.n_rows + (Stream::TR - 1) * experts) / Stream::TR),
           uint32_t((a.n_out + Stream::TC - 1) / Stream::TC)};
       stream_kernel<T><<<dim3(kStreamGroups), dim3(256), 0, s>>>(what);
       return hipGetLastError();
