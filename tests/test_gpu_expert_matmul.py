@@ -229,7 +229,10 @@ def whole_values(rows, cols, filled, seed, per_row=1):
     # rows and columns, experts without rows, several tiles a workgroup
     ([300, 5, 0, 127, 260], 264, 1024), ([1], 8, 512), ([0, 0], 128, 640),
     ([256, 255, 257], 256, 640), ([70, 0, 513], 1096, 896),
-    ([40] * 90, 1032, 512), ([0] * 100 + [200] + [0] * 30, 40, 2176)])
+    ([40] * 90, 1032, 512), ([0] * 100 + [200] + [0] * 30, 40, 2176),
+    ([1500, 0, 900, 257], 1032, 640), ([2000, 700, 33], 704, 1024),
+    ([0] * 10 + [2000] + [0] * 3, 1032, 2176), ([5000, 3200], 2052, 128),
+    ([60] * 8, 300, 3200)])
 def test_matmul(cl, dtype, counts, N, D):
     off = offsets_of(counts)
     E, held = len(counts), int(off[-1])
