@@ -100,12 +100,6 @@ struct Octet {
 };
 
 // ---------------------------------------------------- the 8-bit format ----
-// Largest |x| of finite values, by their bits: comparisons of the bits of
-// non-negative floats are those of the floats. x: the bits of an fp32 value.
-__device__ __forceinline__ uint32_t finite_abs(float x) {
-  const uint32_t b = __float_as_uint(x) & 0x7FFFFFFFu;
-  return b < 0x7F800000u ? b : 0u;
-}
 // The scale byte of a block whose largest finite |x| has the bits `amax`: e +
 // 127 for the smallest e with amax <= 448 * 2^e, 448 = 1.75 * 2^8. A normal
 // amax is m 2^a with 1 <= m < 2, so e is a - 8, or a - 7 where m > 1.75. Below
@@ -179,14 +173,19 @@ __device__ __forceinline__ K row_max(K x) {
   x = larger(x, dpp<kDppHalfMirror>(x, x));
   return larger(x, dpp<kDppMirror>(x, x));
 }
-__device__ __forceinline__ uint32_t row_max_bits(uint32_t x) {
+// over 8 lanes, and over 16
+__device__ __forceinline__ uint32_t eight_max_bits(uint32_t x) {
   const auto step = [](uint32_t v, uint32_t w) { return v > w ? v : w; };
   x = step(x, __builtin_amdgcn_update_dpp(x, x, kDppPair, 0xF, 0xF, false));
   x = step(x, __builtin_amdgcn_update_dpp(x, x, kDppQuad, 0xF, 0xF, false));
-  x = step(x,
-           __builtin_amdgcn_update_dpp(x, x, kDppHalfMirror, 0xF, 0xF, false));
-  return step(x,
-              __builtin_amdgcn_update_dpp(x, x, kDppMirror, 0xF, 0xF, false));
+  return step(
+      x, __builtin_amdgcn_update_dpp(x, x, kDppHalfMirror, 0xF, 0xF, false));
+}
+__device__ __forceinline__ uint32_t row_max_bits(uint32_t x) {
+  x = eight_max_bits(x);
+  const uint32_t y =
+      __builtin_amdgcn_update_dpp(x, x, kDppMirror, 0xF, 0xF, false);
+  return x > y ? x : y;
 }
 template <typename K>
 __device__ __forceinline__ K wave_max(K x) {

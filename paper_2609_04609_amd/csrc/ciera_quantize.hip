@@ -1,6 +1,8 @@
 // Quantisation into the 8-bit format for CDNA4 (gfx950): e4m3 values with a
 // power-of-two scale per 128 values. All three forms are bound by memory: a
 // value costs its read, one multiply and half a conversion instruction.
+#include <type_traits>
+
 #include "ciera_expert.h"
 #include "ciera_expert_dev.h"
 
@@ -8,63 +10,153 @@ namespace ciera {
 
 namespace {
 
-// Eight values as e4m3, in two dwords.
+// The bits of |x|, 16-bit types by pairs: largest values and the values that are not
+// finite, which lie at kInfinite and above, are found on the bits themselves, two
+// values an instruction. Where a wave meets one that is not finite it takes each
+// value's place one by one (`kAny`), which costs twice the instructions.
 template <typename T>
-__device__ __forceinline__ u32x2 octet_e4m3(const Octet<T> &o, float inv) {
+struct Magnitude {
+  static constexpr uint32_t kWords = T::kBytes * 2;  // of eight values
+  static constexpr uint32_t kInfinite =
+      T::kBytes == 4 ? 0x7F800000u : std::is_same_v<T, Bf16> ? 0x7F80u : 0x7C00u;
+  static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+    if constexpr (T::kBytes == 4) return a > b ? a : b;
+    else {
+      typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+      return __builtin_bit_cast(
+          uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a),
+                                              __builtin_bit_cast(u16x2, b)));
+    }
+  }
+  // word i of an octet, without signs
+  static __device__ __forceinline__ uint32_t word(const Octet<T> &o, uint32_t i) {
+    return o.w[i / 4][i % 4] & (T::kBytes == 4 ? 0x7FFFFFFFu : 0x7FFF7FFFu);
+  }
+  static __device__ __forceinline__ uint32_t finite(uint32_t w) {
+    if constexpr (T::kBytes == 4) return w < kInfinite ? w : 0u;
+    else
+      return ((w & 0xFFFFu) < kInfinite ? w & 0xFFFFu : 0u) |
+             (w >> 16 < kInfinite ? w & 0xFFFF0000u : 0u);
+  }
+  static __device__ __forceinline__ bool infinite(uint32_t w) {
+    if constexpr (T::kBytes == 4) return w >= kInfinite;
+    else
+      return w >= kInfinite << 16 || (w & 0xFFFFu) >= kInfinite;
+  }
+  // the bits of the fp32 value of half h of a word (fp32: of the word)
+  static __device__ __forceinline__ uint32_t wide(uint32_t w, uint32_t h) {
+    if constexpr (T::kBytes == 4) return w;
+    else
+      return __float_as_uint(T::to_float(h ? w >> 16 : w & 0xFFFFu));
+  }
+  // the larger half of a word
+  static __device__ __forceinline__ uint32_t one(uint32_t w) {
+    if constexpr (T::kBytes == 4) return w;
+    else
+      return (w >> 16) > (w & 0xFFFFu) ? w >> 16 : w & 0xFFFFu;
+  }
+};
+
+// Eight values as e4m3, in two dwords. ANY: values that are not finite among them.
+template <bool ANY, typename T>
+__device__ __forceinline__ u32x2 octet_e4m3(const Octet<T> &o,
+                                            const float (&inv)[8]) {
   u32x2 r;
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
-    r[h] = pack_e4m3(times(o.get(4 * h), inv), times(o.get(4 * h + 1), inv),
-                     times(o.get(4 * h + 2), inv), times(o.get(4 * h + 3), inv));
+  for (int h = 0; h < 2; ++h) {
+    float v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float x = o.get(4 * h + k);
+      v[k] = ANY ? times(x, inv[4 * h + k]) : x * inv[4 * h + k];
+    }
+    r[h] = pack_e4m3(v[0], v[1], v[2], v[3]);
+  }
   return r;
 }
 template <typename T>
-__device__ __forceinline__ uint32_t octet_amax(const Octet<T> &o) {
+__device__ __forceinline__ u32x2 octet_e4m3(bool any, const Octet<T> &o,
+                                            float inv) {
+  const float same[8] = {inv, inv, inv, inv, inv, inv, inv, inv};
+  return any ? octet_e4m3<true>(o, same) : octet_e4m3<false>(o, same);
+}
+// Largest finite |x| of N octets of this lane, as one value's bits; `any` if a lane
+// of the wave has one that is not finite.
+template <typename T, int N>
+__device__ __forceinline__ uint32_t octets_amax(const Octet<T> (&o)[N],
+                                                bool &any) {
+  using M = Magnitude<T>;
   uint32_t m = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t v = finite_abs(o.get(i));
-    m = v > m ? v : m;
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (uint32_t i = 0; i < M::kWords; ++i) m = M::larger(m, M::word(o[n], i));
+  any = __ballot(M::infinite(m)) != 0;
+  if (any) {
+    m = 0;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (uint32_t i = 0; i < M::kWords; ++i)
+        m = M::larger(m, M::finite(M::word(o[n], i)));
   }
-  return m;
+  return M::wide(M::one(m), 0);
 }
 
 // ----------------------------------------------------------------- rows ----
 // A wave reads a row of x once and writes it to every row that `position`
-// names. 16 lanes hold a block (8 values each), so its maximum is four DPP
-// steps.
+// names: 1024 columns at a time, 16 a lane, so that every store is 16 bytes a lane.
+// Eight lanes hold a block; its maximum is three DPP steps.
 template <typename T>
 __global__ void __launch_bounds__(256) quantize_rows_kernel(QuantRowsArgs a) {
   const uint32_t lane = threadIdx.x & 63;
-  const uint64_t row = uint64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  const uint64_t row = uint64_t(blockIdx.x) * 4 +
+                       __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (row >= a.n_rows) return;
   const uint8_t *x =
       static_cast<const uint8_t *>(a.x) + row * a.row_stride * T::kBytes;
   const uint64_t filled = (a.n_cols + 127) & ~uint64_t(127);
-  const uint64_t blocks = filled / 128;
-  const uint64_t scales = (blocks + 3) & ~uint64_t(3);
-  for (uint64_t from = 0; from < filled; from += 512) {
-    const uint64_t at = from + lane * 8;
-    Octet<T> o;
-    if (at + 8 <= a.n_cols)
-      o.load(x + at * T::kBytes);
-    else
-      o.load_some(x + at * T::kBytes,
-                  at < a.n_cols ? uint32_t(a.n_cols - at) : 0u);
-    const uint32_t byte = scale_byte(row_max_bits(octet_amax(o)));
-    const u32x2 q = octet_e4m3(o, inverse_scale(byte));
-    const uint64_t block = at / 128;
-    for (uint32_t s = 0; s < a.top_k; ++s) {
-      uint64_t to = row;
-      if (a.position) {
-        const int32_t p = a.position[row * a.top_k + s];
-        to = p < 0 ? ~uint64_t(0) : uint64_t(p);
-      }
-      if (to >= a.q_rows) continue;
-      if (at < filled) __builtin_memcpy(a.q + to * a.q_stride + at, &q, 8);
-      if ((lane & 15) == 0 && block < scales)
-        a.scales[to * a.scale_stride + block] =
-            uint8_t(block < blocks ? byte : 127u);
+  const uint64_t scale_bytes = (filled / 128 + 3) & ~uint64_t(3);
+  // lane s: the row of slot s
+  int32_t named = -1;
+  if (!a.position)
+    named = int32_t(row);
+  else if (lane < a.top_k)
+    named = a.position[row * a.top_k + lane];
+  for (uint64_t from = 0; from < filled; from += 1024) {
+    const uint64_t at = from + lane * 16;
+    Octet<T> o[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint64_t c = at + 8 * h;
+      if (c + 8 <= a.n_cols)
+        o[h].load(x + c * T::kBytes);
+      else
+        o[h].load_some(x + c * T::kBytes,
+                       c < a.n_cols ? uint32_t(a.n_cols - c) : 0u);
+    }
+    bool any;
+    const uint32_t byte = scale_byte(eight_max_bits(octets_amax(o, any)));
+    const float inv = inverse_scale(byte);
+    const u32x2 lo = octet_e4m3(any, o[0], inv), hi = octet_e4m3(any, o[1], inv);
+    const u32x4 q = {lo[0], lo[1], hi[0], hi[1]};
+    // the scales of the eight blocks, those past the row's end 127
+    uint32_t s[2] = {0, 0};
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const uint32_t b = __builtin_amdgcn_readlane(byte, 8 * k);
+      s[k / 4] |= (from + 128 * k < filled ? b : 127u) << (8 * (k % 4));
+    }
+    const bool two = from / 128 + 8 <= scale_bytes;
+    for (uint32_t k = 0; k < a.top_k; ++k) {
+      const int32_t to = __builtin_amdgcn_readlane(named, int(k));
+      if (to < 0 || uint64_t(to) >= a.q_rows) continue;
+      if (at < filled)
+        *reinterpret_cast<u32x4 *>(a.q + uint64_t(to) * a.q_stride + at) = q;
+      if (lane < (two ? 2u : 1u))
+        *reinterpret_cast<uint32_t *>(a.scales + uint64_t(to) * a.scale_stride +
+                                      from / 128 + 4 * lane) =
+            lane == 0 ? s[0] : s[1];
     }
   }
 }
@@ -86,7 +178,6 @@ __global__ void __launch_bounds__(256)
   const uint8_t *w =
       static_cast<const uint8_t *>(a.w) + batch * a.n_rows * a.n_cols * T::kBytes;
   Octet<T> o[8];
-  uint32_t m = 0;
 #pragma unroll
   for (uint32_t i = 0; i < 8; ++i) {
     const uint64_t r = r0 + 16 * i;
@@ -96,10 +187,9 @@ __global__ void __launch_bounds__(256)
     else
       o[i].load_some(p, r < a.n_rows && c0 < a.n_cols
                             ? uint32_t(a.n_cols - c0) : 0u);
-    const uint32_t v = octet_amax(o[i]);
-    m = v > m ? v : m;
   }
-  m = row_max_bits(m);
+  bool any;
+  uint32_t m = row_max_bits(octets_amax(o, any));
 #pragma unroll
   for (int d = 16; d < 64; d <<= 1) {
     const uint32_t v = __shfl_xor(m, d, 64);
@@ -114,7 +204,7 @@ __global__ void __launch_bounds__(256)
 #pragma unroll
   for (uint32_t i = 0; i < 8; ++i) {
     const uint64_t r = r0 + 16 * i;
-    const u32x2 q = octet_e4m3(o[i], inv);
+    const u32x2 q = octet_e4m3(any, o[i], inv);
     if (r < a.n_rows)
       __builtin_memcpy(a.q + (batch * a.n_rows + r) * a.q_stride + c0, &q, 8);
     if (a.q_t) __builtin_memcpy(&tile[t / 16 + 16 * i][(t % 16) * 8], &q, 8);
@@ -151,88 +241,143 @@ __global__ void __launch_bounds__(256)
 }
 
 // -------------------------------------------------------------- columns ----
-// A workgroup takes 128 rows of one expert and 128 columns. Block t of the
-// columns belongs to the expert that the running sum of rounded-up row counts
-// puts it in, which every wave finds for itself.
+// Four dwords of four bytes, transposed.
+__device__ __forceinline__ void transpose4(uint32_t &a, uint32_t &b, uint32_t &c,
+                                           uint32_t &d) {
+  const uint32_t ab_lo = __builtin_amdgcn_perm(b, a, 0x05010400u);  // a0 b0 a1 b1
+  const uint32_t ab_hi = __builtin_amdgcn_perm(b, a, 0x07030602u);  // a2 b2 a3 b3
+  const uint32_t cd_lo = __builtin_amdgcn_perm(d, c, 0x05010400u);
+  const uint32_t cd_hi = __builtin_amdgcn_perm(d, c, 0x07030602u);
+  a = __builtin_amdgcn_perm(cd_lo, ab_lo, 0x05040100u);
+  b = __builtin_amdgcn_perm(cd_lo, ab_lo, 0x07060302u);
+  c = __builtin_amdgcn_perm(cd_hi, ab_hi, 0x05040100u);
+  d = __builtin_amdgcn_perm(cd_hi, ab_hi, 0x07060302u);
+}
+
+// A workgroup takes 128 rows of one expert and 128 columns, a thread 8 x 8 of
+// them, which it transposes in registers; LDS puts the columns' pieces of eight
+// bytes together. Block t of the columns belongs to the expert that the running sum
+// of rounded-up row counts puts it in, which every wave finds for itself.
 template <typename T>
 __global__ void __launch_bounds__(256)
     quantize_columns_kernel(QuantColumnsArgs a, uint32_t col_tiles) {
-  __shared__ uint32_t top[16][128];
-  __shared__ uint8_t tile[128][132];
+  __shared__ uint32_t top[4][128];
+  __shared__ float inverse[128];
+  __shared__ uint32_t row_of[128];
+  // column c's piece of rows 8 g on at place g ^ (c / 8 % 16)
+  __shared__ u32x2 tile[128][16];
   const uint32_t t = threadIdx.x, lane = t & 63;
   const uint32_t block = blockIdx.x / col_tiles;
-  const uint32_t c0 = (blockIdx.x % col_tiles) * 128 + (t % 16) * 8;
+  const uint32_t tile_col = (blockIdx.x % col_tiles) * 128;
+  const uint32_t c0 = tile_col + (t % 16) * 8;
   const ExpertTile where = find_tile(a.offsets, a.n_experts,
                                      uint32_t(a.n_rows), block, 7, lane);
   if (where.expert == kNoExpert) return;
+  // the rows' places in x, once for all columns; none: zeros
+  constexpr uint32_t kNone = ~0u;
+  if (t < 128) {
+    const uint32_t p = where.first + t;
+    uint32_t r = p < where.end ? p : kNone;
+    if (r != kNone && a.source) {
+      const int32_t pair = a.source[p];
+      r = pair < 0 ? kNone : uint32_t(pair) / a.top_k;
+    }
+    row_of[t] = r < a.n_x ? r : kNone;
+  }
+  __syncthreads();
   Octet<T> o[8];
-  uint32_t m[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
   for (uint32_t i = 0; i < 8; ++i) {
-    const uint32_t p = where.first + t / 16 + 16 * i;
-    uint64_t r = p;
-    bool held = p < where.end;
-    if (held && a.source) {
-      const int32_t pair = a.source[p];
-      r = uint32_t(pair) / a.top_k;
-      held = pair >= 0;
-    }
-    held = held && r < a.n_x;
+    const uint32_t r = row_of[t / 16 * 8 + i];
     const uint8_t *x = static_cast<const uint8_t *>(a.x) +
-                       (r * a.row_stride + c0) * T::kBytes;
-    if (held && c0 + 8 <= a.n_cols)
+                       (uint64_t(r) * a.row_stride + c0) * T::kBytes;
+    if (r != kNone && c0 + 8 <= a.n_cols)
       o[i].load(x);
     else
-      o[i].load_some(x, held && c0 < a.n_cols ? uint32_t(a.n_cols - c0) : 0u);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const uint32_t v = finite_abs(o[i].get(k));
-      m[k] = v > m[k] ? v : m[k];
-    }
+      o[i].load_some(x, r != kNone && c0 < a.n_cols ? uint32_t(a.n_cols - c0)
+                                                    : 0u);
   }
+  using M = Magnitude<T>;
+  uint32_t m[M::kWords];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) top[t / 16][(t % 16) * 8 + k] = m[k];
+  for (uint32_t w = 0; w < M::kWords; ++w) m[w] = 0;
+#pragma unroll
+  for (uint32_t i = 0; i < 8; ++i)
+#pragma unroll
+    for (uint32_t w = 0; w < M::kWords; ++w)
+      m[w] = M::larger(m[w], M::word(o[i], w));
+  bool any = false;
+#pragma unroll
+  for (uint32_t w = 0; w < M::kWords; ++w) any = any || M::infinite(m[w]);
+  any = __ballot(any) != 0;
+  if (any) {
+#pragma unroll
+    for (uint32_t w = 0; w < M::kWords; ++w) m[w] = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i)
+#pragma unroll
+      for (uint32_t w = 0; w < M::kWords; ++w)
+        m[w] = M::larger(m[w], M::finite(M::word(o[i], w)));
+  }
+  // over the wave's four groups of rows, then over the waves
+#pragma unroll
+  for (uint32_t w = 0; w < M::kWords; ++w) {
+#pragma unroll
+    for (int d = 16; d < 64; d <<= 1)
+      m[w] = M::larger(m[w], __shfl_xor(m[w], d, 64));
+    if (lane < 16) top[t >> 6][lane * M::kWords + w] = m[w];
+  }
   __syncthreads();
+  // a thread a column
+  if (t < 128) {
+    constexpr uint32_t kHalves = T::kBytes == 4 ? 1 : 2;
+    uint32_t word = top[0][t / kHalves];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const uint32_t v = top[r][(t % 16) * 8 + k];
-      m[k] = v > m[k] ? v : m[k];
-    }
+    for (int w = 1; w < 4; ++w) word = M::larger(word, top[w][t / kHalves]);
+    const uint32_t byte = scale_byte(M::wide(word, t % kHalves));
+    inverse[t] = inverse_scale(byte);
+    if (tile_col + t < a.n_cols)
+      a.scales[uint64_t(tile_col + t) * a.scale_stride + block] = uint8_t(byte);
   }
+  __syncthreads();
   float inv[8];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const uint32_t byte = scale_byte(m[k]);
-    inv[k] = inverse_scale(byte);
-    if (t < 16 && c0 + k < a.n_cols)
-      a.scales[(uint64_t(c0) + k) * a.scale_stride + block] = uint8_t(byte);
+  for (int k = 0; k < 8; ++k) inv[k] = inverse[(t % 16) * 8 + k];
+  uint32_t q[8][2];
+  if (any) {
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) {
+      const u32x2 v = octet_e4m3<true>(o[i], inv);
+      q[i][0] = v[0];
+      q[i][1] = v[1];
+    }
+  } else {
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) {
+      const u32x2 v = octet_e4m3<false>(o[i], inv);
+      q[i][0] = v[0];
+      q[i][1] = v[1];
+    }
   }
 #pragma unroll
-  for (uint32_t i = 0; i < 8; ++i) {
-    u32x2 q;
+  for (int h = 0; h < 2; ++h) {
+    transpose4(q[0][h], q[1][h], q[2][h], q[3][h]);
+    transpose4(q[4][h], q[5][h], q[6][h], q[7][h]);
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      q[h] = pack_e4m3(times(o[i].get(4 * h), inv[4 * h]),
-                       times(o[i].get(4 * h + 1), inv[4 * h + 1]),
-                       times(o[i].get(4 * h + 2), inv[4 * h + 2]),
-                       times(o[i].get(4 * h + 3), inv[4 * h + 3]));
-    __builtin_memcpy(&tile[t / 16 + 16 * i][(t % 16) * 8], &q, 8);
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t c = (t % 16) * 8 + 4 * h + k;
+      tile[c][(t / 16) ^ (t % 16)] = u32x2{q[k][h], q[4 + k][h]};
+    }
   }
   __syncthreads();
 #pragma unroll
   for (uint32_t i = 0; i < 4; ++i) {
-    const uint32_t c = t / 8 + 32 * i, r = (t % 8) * 16;
-    const uint64_t col = (blockIdx.x % col_tiles) * 128 + c;
+    const uint32_t c = t / 8 + 32 * i, g = (t % 8) * 2;
+    const uint64_t col = tile_col + c;
     if (col >= a.n_cols) continue;
-    u32x4 q;
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      q[k] = uint32_t(tile[r + 4 * k][c]) | uint32_t(tile[r + 4 * k + 1][c]) << 8 |
-             uint32_t(tile[r + 4 * k + 2][c]) << 16 |
-             uint32_t(tile[r + 4 * k + 3][c]) << 24;
-    __builtin_memcpy(a.q_t + col * a.length + uint64_t(block) * 128 + r, &q, 16);
+    const u32x2 lo = tile[c][g ^ (c / 8)], hi = tile[c][(g + 1) ^ (c / 8)];
+    *reinterpret_cast<u32x4 *>(a.q_t + col * a.length + uint64_t(block) * 128 +
+                               g * 8) = u32x4{lo[0], lo[1], hi[0], hi[1]};
   }
 }
 
