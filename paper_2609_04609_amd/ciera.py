@@ -434,70 +434,73 @@ def update_cache_t(cache, encoded, n_elems, block_elems, ws, fp16=False,
 #
 # Outputs are the caller's, as above. Shapes, types and devices are checked here,
 # since the library sees pointers alone: a mistake raises ValueError before
-# anything is enqueued.
+# anything is enqueued. A call asks everything of its arguments in one expression
+# (`_packed`, `_strided`), some 0.3 us a tensor, and only where that fails goes
+# through them one by one for the words (`_refuse`).
 
 _WIDE = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
-_E4M3 = (torch.float8_e4m3fn,)
-
-
-def _need(ok, what):
-    if not ok:
-        raise ValueError(what)
-
+_E4M3, _INT, _FLOAT, _BYTE = ((torch.float8_e4m3fn,), (torch.int32,),
+                              (torch.float32,), (torch.uint8,))
 
 # the current device's index, asked for directly as the stream is
 _current_device = getattr(torch._C, "_cuda_getDevice",
                           torch.cuda.current_device)
 
 
-def _arg(t, name, dtypes, shape, packed=True):
-    """``t`` as an argument: on the current device, of one of ``dtypes``, of
-    ``shape`` (None: any size), its last dimension contiguous (``packed``: all
-    of it). Only a mistake costs the words for it."""
-    m = t.shape
-    if (t.is_cuda and t.get_device() == _current_device() and
-            t.dtype in dtypes and len(m) == len(shape) and
-            (t.is_contiguous() if packed else
-             m[-1] <= 1 or t.stride(-1) == 1 or t.numel() == 0)):
-        for n, have in zip(shape, m):
-            if n is not None and n != have:
-                break
-        else:
-            return
-    _refuse(t, name, dtypes, shape)
+def _packed(t, dev, dtypes, shape):
+    """Whether ``t`` is contiguous, of ``shape`` and one of ``dtypes`` and on
+    device ``dev`` (an index; the CPU's is -1)."""
+    return (t.get_device() == dev and t.dtype in dtypes and t.shape == shape and
+            t.is_contiguous())
 
 
-def _refuse(t, name, dtypes, shape):
-    _need(t.is_cuda and t.get_device() == _current_device(),
-          f"{name} is on {t.device}, not on the current device")
-    _need(t.dtype in dtypes, f"{name} has type {t.dtype}")
-    _need(t.dim() == len(shape) and
-          all(n is None or n == m for n, m in zip(shape, t.shape)),
-          f"{name} has shape {tuple(t.shape)}, not "
-          f"{tuple('any' if n is None else n for n in shape)}")
-    raise ValueError(f"{name} is not contiguous")
+def _strided(t, dev, dtypes, shape):
+    """The same for a matrix whose rows may be apart, by ``stride(0)``."""
+    return (t.get_device() == dev and t.dtype in dtypes and t.shape == shape and
+            (t.is_contiguous() or
+             (len(shape) == 2 and (shape[1] <= 1 or t.stride(1) == 1) and
+              (shape[0] <= 1 or t.stride(0) >= shape[1]))))
 
 
-def _row_stride(t, name):
-    """Elements from a row of a matrix to the next."""
+def _refuse(dev, *args):
+    """Say which of (tensor, name, types, shape, check) does not fit."""
+    for t, name, dtypes, shape, check in args:
+        if t is None or check(t, dev, dtypes, shape):
+            continue
+        if t.get_device() != dev:
+            raise ValueError(f"{name} is on {t.device}, not on the current "
+                             "device")
+        if t.dtype not in dtypes:
+            raise ValueError(f"{name} has type {t.dtype}")
+        if t.shape != shape:
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, not "
+                             f"{tuple(shape)}")
+        raise ValueError(f"{name} is not contiguous")
+    raise ValueError("arguments do not fit each other")
+
+
+def _device(t, name):
+    """The current device's index, for a call whose first tensor is ``t``."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} is on {t.device}, not on the current device")
+    return _current_device()
+
+
+def _dims(t, name, n):
+    """The shape of a tensor of ``n`` dimensions."""
+    if t.dim() != n:
+        raise ValueError(f"{name} has {t.dim()} dimensions, not {n}")
+    return t.shape
+
+
+def _row_stride(t):
+    """Elements from a row of a checked matrix to the next."""
     rows, cols = t.shape
-    if rows <= 1 or cols == 0:
-        return cols or 1
-    stride = t.stride(0)
-    if stride < cols:
-        raise ValueError(f"the rows of {name} overlap")
-    return stride
+    return t.stride(0) if rows > 1 and cols > 0 else cols or 1
 
 
-_INT, _FLOAT, _BYTE = (torch.int32,), (torch.float32,), (torch.uint8,)
-
-
-def _ints(t, name, *shape):
-    _arg(t, name, _INT, shape)
-
-
-def _floats(t, name, *shape):
-    _arg(t, name, _FLOAT, shape)
+def _scales_fit(s, filled):
+    return s.shape[-1] * 128 >= filled
 
 
 def quantized_shapes(rows, cols):
@@ -508,51 +511,53 @@ def quantized_shapes(rows, cols):
     return (rows, 128 * blocks), (rows, -(-blocks // 4) * 4)
 
 
-def _narrow(q, s, name, rows, filled, packed=True):
-    """An 8-bit matrix of ``rows`` rows and its scales."""
-    _arg(q, name, _E4M3, (rows, filled), packed)
-    _arg(s, "scales of " + name, _BYTE, (rows, None), packed)
-    if q.shape[1] % 128 or s.shape[1] < q.shape[1] // 128:
-        raise ValueError(f"{name} has rows of {q.shape[1]} bytes and "
-                         f"{s.shape[1]} scales")
-
-
 def route_t(logits, expert_ids, weights, bias=None, groups=1, top_groups=1,
             group_top_two=False, sigmoid=False, normalize=False, scale=1.0):
     """Choose experts: ``logits`` [T, E] -> ``expert_ids`` int32 and
     ``weights`` fp32, both [T, k]; ``bias`` fp32 [E]."""
-    _arg(logits, "logits", _WIDE, (None, None), packed=False)
-    T, E = logits.shape
-    _ints(expert_ids, "expert_ids", T, None)
-    _floats(weights, "weights", T, expert_ids.shape[1])
-    if bias is not None:
-        _floats(bias, "bias", E)
+    T, E = _dims(logits, "logits", 2)
+    k = _dims(expert_ids, "expert_ids", 2)[1]
+    dev = _device(logits, "logits")
+    if not (_strided(logits, dev, _WIDE, (T, E)) and
+            _packed(expert_ids, dev, _INT, (T, k)) and
+            _packed(weights, dev, _FLOAT, (T, k)) and
+            (bias is None or _packed(bias, dev, _FLOAT, (E,)))):
+        _refuse(dev, (logits, "logits", _WIDE, (T, E), _strided),
+                (expert_ids, "expert_ids", _INT, (T, k), _packed),
+                (weights, "weights", _FLOAT, (T, k), _packed),
+                (bias, "bias", _FLOAT, (E,), _packed))
     flags = ((ROUTE_SIGMOID if sigmoid else 0) |
              (ROUTE_NORMALIZE if normalize else 0) |
              (ROUTE_GROUP_TOP_TWO if group_top_two else 0))
-    rc = ciera_route(_ptr(logits), _WIDE[logits.dtype], T, E,
-                     _row_stride(logits, "logits"), _ptr(bias), groups,
-                     top_groups, expert_ids.shape[1], flags, scale,
-                     _ptr(expert_ids), _ptr(weights), _stream())
+    rc = ciera_route(logits.data_ptr(), _WIDE[logits.dtype], T, E,
+                     _row_stride(logits), _ptr(bias), groups, top_groups, k,
+                     flags, scale, expert_ids.data_ptr(), weights.data_ptr(),
+                     _stream())
     return _check("ciera_route", rc)
 
 
 def route_backward_t(logits, expert_ids, d_weights, d_logits, sigmoid=False,
                      normalize=False, scale=1.0):
     """Gradient of route_t's weights -> gradient of its logits."""
-    _arg(logits, "logits", _WIDE, (None, None), packed=False)
-    T, E = logits.shape
-    _ints(expert_ids, "expert_ids", T, None)
-    k = expert_ids.shape[1]
-    _floats(d_weights, "d_weights", T, k)
-    _arg(d_logits, "d_logits", (logits.dtype,), (T, E), packed=False)
+    T, E = _dims(logits, "logits", 2)
+    k = _dims(expert_ids, "expert_ids", 2)[1]
+    dev = _device(logits, "logits")
+    same = (logits.dtype,)
+    if not (_strided(logits, dev, _WIDE, (T, E)) and
+            _packed(expert_ids, dev, _INT, (T, k)) and
+            _packed(d_weights, dev, _FLOAT, (T, k)) and
+            _strided(d_logits, dev, same, (T, E))):
+        _refuse(dev, (logits, "logits", _WIDE, (T, E), _strided),
+                (expert_ids, "expert_ids", _INT, (T, k), _packed),
+                (d_weights, "d_weights", _FLOAT, (T, k), _packed),
+                (d_logits, "d_logits", same, (T, E), _strided))
     flags = ((ROUTE_SIGMOID if sigmoid else 0) |
              (ROUTE_NORMALIZE if normalize else 0))
-    rc = ciera_route_backward(_ptr(logits), _WIDE[logits.dtype], T, E,
-                              _row_stride(logits, "logits"), k, flags, scale,
-                              _ptr(expert_ids), _ptr(d_weights),
-                              _ptr(d_logits),
-                              _row_stride(d_logits, "d_logits"), _stream())
+    rc = ciera_route_backward(logits.data_ptr(), _WIDE[logits.dtype], T, E,
+                              _row_stride(logits), k, flags, scale,
+                              expert_ids.data_ptr(), d_weights.data_ptr(),
+                              d_logits.data_ptr(), _row_stride(d_logits),
+                              _stream())
     return _check("ciera_route_backward", rc)
 
 
@@ -571,15 +576,22 @@ def route_plan_t(expert_ids, n_experts, offsets, source, position, ws,
                  first_expert=0):
     """Sort the (token, slot) pairs of ``expert_ids`` [T, k] by expert:
     ``offsets`` [n_experts + 1], ``source`` [T k], ``position`` [T, k]."""
-    _ints(expert_ids, "expert_ids", None, None)
-    T, k = expert_ids.shape
-    _ints(offsets, "offsets", n_experts + 1)
-    _ints(source, "source", T * k)
-    _ints(position, "position", T, k)
-    _arg(ws.buf, "the workspace", _BYTE, (None,))
-    rc = ciera_route_plan(_ptr(expert_ids), T, k, first_expert, n_experts,
-                          _ptr(offsets), _ptr(source), _ptr(position),
-                          _ptr(ws.buf), ws.nbytes, _stream())
+    T, k = _dims(expert_ids, "expert_ids", 2)
+    dev = _device(expert_ids, "expert_ids")
+    if not (_packed(expert_ids, dev, _INT, (T, k)) and
+            _packed(offsets, dev, _INT, (n_experts + 1,)) and
+            _packed(source, dev, _INT, (T * k,)) and
+            _packed(position, dev, _INT, (T, k)) and
+            ws.buf.get_device() == dev):
+        _refuse(dev, (expert_ids, "expert_ids", _INT, (T, k), _packed),
+                (offsets, "offsets", _INT, (n_experts + 1,), _packed),
+                (source, "source", _INT, (T * k,), _packed),
+                (position, "position", _INT, (T, k), _packed),
+                (ws.buf, "the workspace", _BYTE, (ws.nbytes,), _packed))
+    rc = ciera_route_plan(expert_ids.data_ptr(), T, k, first_expert, n_experts,
+                          offsets.data_ptr(), source.data_ptr(),
+                          position.data_ptr(), ws.buf.data_ptr(), ws.nbytes,
+                          _stream())
     return _check("ciera_route_plan", rc)
 
 
@@ -587,18 +599,25 @@ def quantize_rows_t(x, q, scales, position=None):
     """``x`` [R, C] -> 8-bit rows with a scale per 1 x 128 block: row r to row
     r, or with ``position`` [R, k] to the k rows that it names. ``q`` and
     ``scales`` have the shapes of quantized_shapes()."""
-    _arg(x, "x", _WIDE, (None, None), packed=False)
-    R, C = x.shape
-    _narrow(q, scales, "q", None, -(-C // 128) * 128)
-    _need(scales.shape[0] == q.shape[0], "q and its scales differ in rows")
-    k = 1
-    if position is not None:
-        _ints(position, "position", R, None)
-        k = position.shape[1]
-    rc = ciera_quantize_rows(_ptr(x), _WIDE[x.dtype], R, C,
-                             _row_stride(x, "x"), _ptr(position), k,
-                             q.shape[0], _ptr(q), q.shape[1], _ptr(scales),
-                             scales.shape[1], _stream())
+    R, C = _dims(x, "x", 2)
+    Q = _dims(q, "q", 2)[0]
+    filled = -(-C // 128) * 128
+    S = _dims(scales, "scales of q", 2)[1]
+    k = 1 if position is None else _dims(position, "position", 2)[1]
+    dev = _device(x, "x")
+    if not (_strided(x, dev, _WIDE, (R, C)) and
+            _packed(q, dev, _E4M3, (Q, filled)) and
+            _packed(scales, dev, _BYTE, (Q, S)) and
+            _scales_fit(scales, filled) and
+            (position is None or _packed(position, dev, _INT, (R, k)))):
+        _refuse(dev, (x, "x", _WIDE, (R, C), _strided),
+                (q, "q", _E4M3, (Q, filled), _packed),
+                (scales, "scales of q", _BYTE, (Q, S), _packed),
+                (position, "position", _INT, (R, k), _packed))
+    rc = ciera_quantize_rows(x.data_ptr(), _WIDE[x.dtype], R, C,
+                             _row_stride(x), _ptr(position), k, Q,
+                             q.data_ptr(), filled, scales.data_ptr(), S,
+                             _stream())
     return _check("ciera_quantize_rows", rc)
 
 
@@ -606,25 +625,30 @@ def quantize_blocks_t(w, q, scales, q_t=None, scales_t=None):
     """``w`` [E, N, C] -> 8-bit with a scale per 128 x 128 block, and with
     ``q_t`` and ``scales_t`` the transpose [E, C, N] too. Shapes: those of
     quantized_shapes() of a matrix, with one scale row per 128 rows."""
-    _arg(w, "w", _WIDE, (None, None, None))
-    E, N, C = w.shape
+    E, N, C = _dims(w, "w", 3)
     nb, cb = -(-N // 128), -(-C // 128)
-
-    def pair(q, s, name, rows, blocks, filled):
-        _arg(q, name, _E4M3, (E, rows, filled))
-        _arg(s, "scales of " + name, _BYTE, (E, blocks, None))
-
-    pair(q, scales, "q", N, nb, 128 * cb)
-    _need((q_t is None) == (scales_t is None),
-          "q_t and scales_t go together")
-    qt_stride = st_stride = 0
-    if q_t is not None:
-        pair(q_t, scales_t, "q_t", C, cb, 128 * nb)
-        qt_stride, st_stride = q_t.shape[2], scales_t.shape[2]
-    rc = ciera_quantize_blocks(_ptr(w), _WIDE[w.dtype], E, N, C, _ptr(q),
-                               q.shape[2], _ptr(scales), scales.shape[2],
-                               _ptr(q_t), qt_stride, _ptr(scales_t),
-                               st_stride, _stream())
+    if (q_t is None) != (scales_t is None):
+        raise ValueError("q_t and scales_t go together")
+    S = _dims(scales, "scales of q", 3)[2]
+    St = 0 if q_t is None else _dims(scales_t, "scales of q_t", 3)[2]
+    dev = _device(w, "w")
+    if not (_packed(w, dev, _WIDE, (E, N, C)) and
+            _packed(q, dev, _E4M3, (E, N, 128 * cb)) and
+            _packed(scales, dev, _BYTE, (E, nb, S)) and
+            _scales_fit(scales, 128 * cb) and
+            (q_t is None or
+             (_packed(q_t, dev, _E4M3, (E, C, 128 * nb)) and
+              _packed(scales_t, dev, _BYTE, (E, cb, St)) and
+              _scales_fit(scales_t, 128 * nb)))):
+        _refuse(dev, (w, "w", _WIDE, (E, N, C), _packed),
+                (q, "q", _E4M3, (E, N, 128 * cb), _packed),
+                (scales, "scales of q", _BYTE, (E, nb, S), _packed),
+                (q_t, "q_t", _E4M3, (E, C, 128 * nb), _packed),
+                (scales_t, "scales of q_t", _BYTE, (E, cb, St), _packed))
+    rc = ciera_quantize_blocks(w.data_ptr(), _WIDE[w.dtype], E, N, C,
+                               q.data_ptr(), 128 * cb, scales.data_ptr(), S,
+                               _ptr(q_t), 128 * nb, _ptr(scales_t), St,
+                               _stream())
     return _check("ciera_quantize_blocks", rc)
 
 
@@ -633,20 +657,27 @@ def quantize_columns_t(x, offsets, q_t, scales_t, source=None, top_k=1):
     expert's rows filled up to a multiple of 128: ``q_t`` [C, L], L at least
     ciera_columns_length(). Sorted row p is row p of ``x``, or with ``source``
     row source[p] // top_k."""
-    _arg(x, "x", _WIDE, (None, None), packed=False)
-    R, C = x.shape
-    _ints(offsets, "offsets", None)
-    _need(offsets.shape[0] >= 2, "offsets holds no expert")
-    P = R
-    if source is not None:
-        _ints(source, "source", None)
-        P = source.shape[0]
-    _narrow(q_t, scales_t, "q_t", C, None)
-    rc = ciera_quantize_columns(_ptr(x), _WIDE[x.dtype], R, P, C,
-                                _row_stride(x, "x"), _ptr(source), top_k,
-                                _ptr(offsets), offsets.shape[0] - 1,
-                                _ptr(q_t), q_t.shape[1], _ptr(scales_t),
-                                scales_t.shape[1], _stream())
+    R, C = _dims(x, "x", 2)
+    E = _dims(offsets, "offsets", 1)[0] - 1
+    L = _dims(q_t, "q_t", 2)[1]
+    S = _dims(scales_t, "scales of q_t", 2)[1]
+    P = R if source is None else _dims(source, "source", 1)[0]
+    dev = _device(x, "x")
+    if not (_strided(x, dev, _WIDE, (R, C)) and E >= 1 and
+            _packed(offsets, dev, _INT, (E + 1,)) and
+            _packed(q_t, dev, _E4M3, (C, L)) and
+            _packed(scales_t, dev, _BYTE, (C, S)) and
+            _scales_fit(scales_t, L) and
+            (source is None or _packed(source, dev, _INT, (P,)))):
+        _refuse(dev, (x, "x", _WIDE, (R, C), _strided),
+                (offsets, "offsets", _INT, (max(E, 1) + 1,), _packed),
+                (q_t, "q_t", _E4M3, (C, L), _packed),
+                (scales_t, "scales of q_t", _BYTE, (C, S), _packed),
+                (source, "source", _INT, (P,), _packed))
+    rc = ciera_quantize_columns(x.data_ptr(), _WIDE[x.dtype], R, P, C,
+                                _row_stride(x), _ptr(source), top_k,
+                                offsets.data_ptr(), E, q_t.data_ptr(), L,
+                                scales_t.data_ptr(), S, _stream())
     return _check("ciera_quantize_columns", rc)
 
 
@@ -654,36 +685,57 @@ def expert_matmul_t(a, a_scales, b, b_scales, offsets, out):
     """8-bit rows ``a`` [P, D] times the 8-bit weights ``b`` [E, N, D] of their
     experts -> ``out`` [P, N]; ``offsets`` int32 [E + 1], or None for one
     expert."""
-    _narrow(a, a_scales, "a", None, None, packed=False)
-    P, D = a.shape
-    _need(a_scales.shape[0] == P, "a and its scales differ in rows")
-    _arg(b, "b", _E4M3, (None, None, D))
-    E, N, _ = b.shape
-    _arg(b_scales, "scales of b", _BYTE, (E, -(-N // 128), None))
-    _arg(out, "out", _WIDE, (P, N), packed=False)
-    if offsets is not None:
-        _ints(offsets, "offsets", E + 1)
-    rc = ciera_expert_matmul(_ptr(a), _row_stride(a, "a"), _ptr(a_scales),
-                             _row_stride(a_scales, "scales of a"), P, _ptr(b),
-                             D, _ptr(b_scales), b_scales.shape[2], E, N, D,
-                             _ptr(offsets), _ptr(out), _WIDE[out.dtype],
-                             _row_stride(out, "out"), _stream())
+    P, D = _dims(a, "a", 2)
+    E, N = _dims(b, "b", 3)[:2]
+    Sa = _dims(a_scales, "scales of a", 2)[1]
+    Sb = _dims(b_scales, "scales of b", 3)[2]
+    nb = -(-N // 128)
+    dev = _device(a, "a")
+    if not (_strided(a, dev, _E4M3, (P, D)) and
+            _strided(a_scales, dev, _BYTE, (P, Sa)) and
+            _packed(b, dev, _E4M3, (E, N, D)) and
+            _packed(b_scales, dev, _BYTE, (E, nb, Sb)) and
+            _scales_fit(a_scales, D) and _scales_fit(b_scales, D) and
+            _strided(out, dev, _WIDE, (P, N)) and
+            (offsets is None or _packed(offsets, dev, _INT, (E + 1,)))):
+        _refuse(dev, (a, "a", _E4M3, (P, D), _strided),
+                (a_scales, "scales of a", _BYTE, (P, Sa), _strided),
+                (b, "b", _E4M3, (E, N, D), _packed),
+                (b_scales, "scales of b", _BYTE, (E, nb, Sb), _packed),
+                (out, "out", _WIDE, (P, N), _strided),
+                (offsets, "offsets", _INT, (E + 1,), _packed))
+    rc = ciera_expert_matmul(a.data_ptr(), _row_stride(a),
+                             a_scales.data_ptr(), _row_stride(a_scales), P,
+                             b.data_ptr(), D, b_scales.data_ptr(), Sb, E, N, D,
+                             _ptr(offsets), out.data_ptr(), _WIDE[out.dtype],
+                             _row_stride(out), _stream())
     return _check("ciera_expert_matmul", rc)
 
 
 def expert_weight_grad_t(dy_t, dy_scales, x_t, x_scales, offsets, d_w):
     """The experts' weight gradients ``d_w`` [E, N, C] from the 8-bit columns
     ``dy_t`` [N, L] and ``x_t`` [C, L] of quantize_columns_t."""
-    _arg(d_w, "d_w", _WIDE, (None, None, None))
-    E, N, C = d_w.shape
-    _narrow(dy_t, dy_scales, "dy_t", N, None)
-    L = dy_t.shape[1]
-    _narrow(x_t, x_scales, "x_t", C, L)
-    _ints(offsets, "offsets", E + 1)
-    rc = ciera_expert_weight_grad(_ptr(dy_t), _ptr(dy_scales),
-                                  dy_scales.shape[1], _ptr(x_t),
-                                  _ptr(x_scales), x_scales.shape[1], L, E, N,
-                                  C, _ptr(offsets), _ptr(d_w),
+    E, N, C = _dims(d_w, "d_w", 3)
+    L = _dims(dy_t, "dy_t", 2)[1]
+    Sy = _dims(dy_scales, "scales of dy_t", 2)[1]
+    Sx = _dims(x_scales, "scales of x_t", 2)[1]
+    dev = _device(dy_t, "dy_t")
+    if not (_packed(dy_t, dev, _E4M3, (N, L)) and
+            _packed(dy_scales, dev, _BYTE, (N, Sy)) and
+            _packed(x_t, dev, _E4M3, (C, L)) and
+            _packed(x_scales, dev, _BYTE, (C, Sx)) and
+            _scales_fit(dy_scales, L) and _scales_fit(x_scales, L) and
+            _packed(offsets, dev, _INT, (E + 1,)) and
+            _packed(d_w, dev, _WIDE, (E, N, C))):
+        _refuse(dev, (dy_t, "dy_t", _E4M3, (N, L), _packed),
+                (dy_scales, "scales of dy_t", _BYTE, (N, Sy), _packed),
+                (x_t, "x_t", _E4M3, (C, L), _packed),
+                (x_scales, "scales of x_t", _BYTE, (C, Sx), _packed),
+                (offsets, "offsets", _INT, (E + 1,), _packed),
+                (d_w, "d_w", _WIDE, (E, N, C), _packed))
+    rc = ciera_expert_weight_grad(dy_t.data_ptr(), dy_scales.data_ptr(), Sy,
+                                  x_t.data_ptr(), x_scales.data_ptr(), Sx, L,
+                                  E, N, C, offsets.data_ptr(), d_w.data_ptr(),
                                   _WIDE[d_w.dtype], _stream())
     return _check("ciera_expert_weight_grad", rc)
 
@@ -691,33 +743,45 @@ def expert_weight_grad_t(dy_t, dy_scales, x_t, x_scales, offsets, d_w):
 def combine_t(rows, position, out, weights=None):
     """``out`` [T, C]: for every token the sum of the rows [P, C] that
     ``position`` [T, k] names, times ``weights`` [T, k] if given."""
-    _arg(rows, "rows", _WIDE, (None, None), packed=False)
-    P, C = rows.shape
-    _ints(position, "position", None, None)
-    T, k = position.shape
-    _arg(out, "out", (rows.dtype,), (T, C), packed=False)
-    if weights is not None:
-        _floats(weights, "weights", T, k)
-    rc = ciera_combine(_ptr(rows), _WIDE[rows.dtype], P, C,
-                       _row_stride(rows, "rows"), _ptr(weights),
-                       _ptr(position), T, k, _ptr(out),
-                       _row_stride(out, "out"), _stream())
+    P, C = _dims(rows, "rows", 2)
+    T, k = _dims(position, "position", 2)
+    dev = _device(rows, "rows")
+    same = (rows.dtype,)
+    if not (_strided(rows, dev, _WIDE, (P, C)) and
+            _packed(position, dev, _INT, (T, k)) and
+            _strided(out, dev, same, (T, C)) and
+            (weights is None or _packed(weights, dev, _FLOAT, (T, k)))):
+        _refuse(dev, (rows, "rows", _WIDE, (P, C), _strided),
+                (position, "position", _INT, (T, k), _packed),
+                (out, "out", same, (T, C), _strided),
+                (weights, "weights", _FLOAT, (T, k), _packed))
+    rc = ciera_combine(rows.data_ptr(), _WIDE[rows.dtype], P, C,
+                       _row_stride(rows), _ptr(weights), position.data_ptr(),
+                       T, k, out.data_ptr(), _row_stride(out), _stream())
     return _check("ciera_combine", rc)
 
 
 def combine_backward_t(d_out, rows, weights, position, d_rows, d_weights):
     """Gradients of combine_t: ``d_rows`` [P, C] and ``d_weights`` [T, k]."""
-    _arg(rows, "rows", _WIDE, (None, None), packed=False)
-    P, C = rows.shape
-    _ints(position, "position", None, None)
-    T, k = position.shape
-    _arg(d_out, "d_out", (rows.dtype,), (T, C), packed=False)
-    _floats(weights, "weights", T, k)
-    _arg(d_rows, "d_rows", (rows.dtype,), (P, C), packed=False)
-    _floats(d_weights, "d_weights", T, k)
+    P, C = _dims(rows, "rows", 2)
+    T, k = _dims(position, "position", 2)
+    dev = _device(rows, "rows")
+    same = (rows.dtype,)
+    if not (_strided(rows, dev, _WIDE, (P, C)) and
+            _packed(position, dev, _INT, (T, k)) and
+            _strided(d_out, dev, same, (T, C)) and
+            _packed(weights, dev, _FLOAT, (T, k)) and
+            _strided(d_rows, dev, same, (P, C)) and
+            _packed(d_weights, dev, _FLOAT, (T, k))):
+        _refuse(dev, (rows, "rows", _WIDE, (P, C), _strided),
+                (position, "position", _INT, (T, k), _packed),
+                (d_out, "d_out", same, (T, C), _strided),
+                (weights, "weights", _FLOAT, (T, k), _packed),
+                (d_rows, "d_rows", same, (P, C), _strided),
+                (d_weights, "d_weights", _FLOAT, (T, k), _packed))
     rc = ciera_combine_backward(
-        _ptr(d_out), _row_stride(d_out, "d_out"), _ptr(rows),
-        _WIDE[rows.dtype], P, C, _row_stride(rows, "rows"), _ptr(weights),
-        _ptr(position), T, k, _ptr(d_rows), _row_stride(d_rows, "d_rows"),
-        _ptr(d_weights), _stream())
+        d_out.data_ptr(), _row_stride(d_out), rows.data_ptr(),
+        _WIDE[rows.dtype], P, C, _row_stride(rows), weights.data_ptr(),
+        position.data_ptr(), T, k, d_rows.data_ptr(), _row_stride(d_rows),
+        d_weights.data_ptr(), _stream())
     return _check("ciera_combine_backward", rc)

@@ -495,3 +495,74 @@ def test_combine_of_differences(cl):
         moved = loss(rows, w + dw) - base
         expect = float((d_w.cpu().double() * dw.double()).sum())
         assert abs(moved - expect) <= 1e-3 * T * C ** 0.5
+
+
+# -------------------------------------------------------------- refusals ----
+
+def test_tensors_that_do_not_fit(cl):
+    """Every call names the tensor that does not fit; nothing is enqueued."""
+    T, k, E, C, P = 4, 2, 3, 256, 8
+    f = torch.zeros(T, C, device=DEV)
+    i = torch.zeros(T, k, dtype=torch.int32, device=DEV)
+    w = torch.zeros(T, k, device=DEV)
+    off = torch.zeros(E + 1, dtype=torch.int32, device=DEV)
+    rows = torch.zeros(P, C, device=DEV)
+    q, s = narrow(P, C)
+    b = torch.zeros(E, 128, C, device=DEV).to(E4M3)
+    sb = torch.zeros(E, 1, 4, dtype=torch.uint8, device=DEV)
+    qt, st = narrow(C, 512)
+    dw = torch.zeros(E, C, C, device=DEV)
+    out = torch.zeros(P, 128, device=DEV)
+    bad = [
+        ("weights has type", lambda: cl.route_t(f, i, w.half())),
+        ("weights has shape", lambda: cl.route_t(f, i, w[:3])),
+        ("expert_ids has type", lambda: cl.route_t(f, i.long(), w)),
+        ("logits is not contiguous", lambda: cl.route_t(f.t()[:T], i, w)),
+        ("logits is not contiguous",
+         lambda: cl.route_t(f[:1].expand(T, C), i, w)),
+        ("bias has shape", lambda: cl.route_t(f, i, w, bias=f[0, :5])),
+        ("bias is on cpu", lambda: cl.route_t(f, i, w, bias=torch.zeros(C))),
+        ("d_logits has type",
+         lambda: cl.route_backward_t(f, i, w, f.half())),
+        ("offsets has shape", lambda: cl.route_plan_t(
+            i, E, off[:3], i.view(-1), i, cl.PlanWorkspace(T, k, E))),
+        ("position has shape",
+         lambda: cl.quantize_rows_t(f, q, s, position=i[:2])),
+        ("q has shape", lambda: cl.quantize_rows_t(f[:, :100], q, s)),
+        ("do not fit", lambda: cl.quantize_rows_t(f, q, s[:, :1].contiguous())),
+        ("w is not contiguous",
+         lambda: cl.quantize_blocks_t(dw.transpose(1, 2), b, sb)),
+        ("go together",
+         lambda: cl.quantize_blocks_t(dw, b, sb, q_t=b)),
+        ("offsets has shape",
+         lambda: cl.quantize_columns_t(rows, off[:1], qt, st)),
+        ("scales of b has shape",
+         lambda: cl.expert_matmul_t(q, s, b, sb[:2], off, out)),
+        ("out has shape", lambda: cl.expert_matmul_t(q, s, b, sb, off, rows)),
+        ("offsets has type",
+         lambda: cl.expert_matmul_t(q, s, b, sb, off.long(), out)),
+        ("x_t has shape",
+         lambda: cl.expert_weight_grad_t(qt, st, qt[:5], st, off, dw)),
+        ("out has type",
+         lambda: cl.combine_t(rows, i, f.half())),
+        ("d_rows has shape",
+         lambda: cl.combine_backward_t(f, rows, w, i, rows[:3], w)),
+    ]
+    for what, call in bad:
+        with pytest.raises(ValueError, match=what):
+            call()
+    with pytest.raises(cl.CieraError):  # one expert's rows need no offsets
+        cl.expert_matmul_t(q, s, b, sb, None, out)
+    with pytest.raises(cl.CieraError):  # more experts a token than experts
+        cl.route_t(f[:, :1].contiguous(), i, w)
+
+
+def test_one_column_and_one_row_views(cl):
+    """Matrices of one column or row keep their strides."""
+    wide = randn(6, 9, seed=1).to(DEV)
+    pos = torch.arange(6, dtype=torch.int32, device=DEV).view(3, 2)
+    out = torch.full((3, 4), 7.0, device=DEV)
+    cl.combine_t(wide[:, 2:3], pos, out[:, 1:2])
+    y = wide[:, 2].view(3, 2).sum(1)
+    assert torch.equal(out[:, 1], y) and (out[:, 0] == 7).all()
+    assert (out[:, 2:] == 7).all()

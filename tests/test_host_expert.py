@@ -166,6 +166,8 @@ def test_tensors_are_checked(cl):
         cl.route_t(x, i, w)
     with pytest.raises(ValueError, match="rows is on cpu"):
         cl.combine_t(x, i, x)
+    with pytest.raises(ValueError, match="logits has 1 dimensions"):
+        cl.route_t(x[0], i, w)
 
 
 def test_the_reference_itself():
