@@ -157,49 +157,73 @@ __device__ __forceinline__ double lane_of(double x, int lane) {
   return __longlong_as_double((long long)(uint64_t(hi) << 32 | lo));
 }
 
+// Whole numbers of 32 and 64 bits. 0, or a lane without a source, is the least:
+// a maximum takes the other lane's value in one instruction.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_or_zero(uint32_t x) {
+  return uint32_t(
+      __builtin_amdgcn_update_dpp(0, int(x), CTRL, 0xF, 0xF, false));
+}
+template <int CTRL>
+__device__ __forceinline__ uint64_t dpp_or_zero(uint64_t x) {
+  return uint64_t(dpp_or_zero<CTRL>(uint32_t(x >> 32))) << 32 |
+         dpp_or_zero<CTRL>(uint32_t(x));
+}
+__device__ __forceinline__ uint32_t lane_of(uint32_t x, int lane) {
+  return uint32_t(__builtin_amdgcn_readlane(int(x), lane));
+}
+__device__ __forceinline__ uint64_t lane_of(uint64_t x, int lane) {
+  return uint64_t(lane_of(uint32_t(x >> 32), lane)) << 32 |
+         lane_of(uint32_t(x), lane);
+}
 template <typename K>
 __device__ __forceinline__ K larger(K a, K b) {
   return a > b ? a : b;
 }
-__device__ __forceinline__ float larger(float a, float b) {
-  return __builtin_fmaxf(a, b);
+// over 8 lanes, over the 16 of a row, in every lane; and over the wave
+template <typename O>
+__device__ __forceinline__ O eight_max(O x) {
+  x = larger(x, dpp_or_zero<kDppPair>(x));
+  x = larger(x, dpp_or_zero<kDppQuad>(x));
+  return larger(x, dpp_or_zero<kDppHalfMirror>(x));
 }
-
-// over the 16 lanes of a row, in every lane
-template <typename K>
-__device__ __forceinline__ K row_max(K x) {
-  x = larger(x, dpp<kDppPair>(x, x));
-  x = larger(x, dpp<kDppQuad>(x, x));
-  x = larger(x, dpp<kDppHalfMirror>(x, x));
-  return larger(x, dpp<kDppMirror>(x, x));
+template <typename O>
+__device__ __forceinline__ O row_max(O x) {
+  x = eight_max(x);
+  return larger(x, dpp_or_zero<kDppMirror>(x));
 }
-// over 8 lanes, and over 16
-__device__ __forceinline__ uint32_t eight_max_bits(uint32_t x) {
-  const auto step = [](uint32_t v, uint32_t w) { return v > w ? v : w; };
-  x = step(x, __builtin_amdgcn_update_dpp(x, x, kDppPair, 0xF, 0xF, false));
-  x = step(x, __builtin_amdgcn_update_dpp(x, x, kDppQuad, 0xF, 0xF, false));
-  return step(
-      x, __builtin_amdgcn_update_dpp(x, x, kDppHalfMirror, 0xF, 0xF, false));
-}
-__device__ __forceinline__ uint32_t row_max_bits(uint32_t x) {
-  x = eight_max_bits(x);
-  const uint32_t y =
-      __builtin_amdgcn_update_dpp(x, x, kDppMirror, 0xF, 0xF, false);
-  return x > y ? x : y;
-}
-template <typename K>
-__device__ __forceinline__ K wave_max(K x) {
+template <typename O>
+__device__ __forceinline__ O wave_max(O x) {
   x = row_max(x);
-  x = larger(x, dpp<kDppBcast15>(x, x));
-  x = larger(x, dpp<kDppBcast31>(x, x));
+  x = larger(x, dpp_or_zero<kDppBcast15>(x));
+  x = larger(x, dpp_or_zero<kDppBcast31>(x));
   return lane_of(x, 63);
+}
+// Floats as whole numbers of the same order (no NaN; -0 as 0), and back.
+__device__ __forceinline__ uint32_t to_order(float x) {
+  const uint32_t b = __float_as_uint(x + 0.0f);
+  return b ^ (uint32_t(int(b) >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ uint64_t to_order(double x) {
+  const uint64_t b = uint64_t(__double_as_longlong(x + 0.0));
+  return b ^ (uint64_t((long long)(b) >> 63) | 0x8000000000000000ull);
+}
+__device__ __forceinline__ float from_order(uint32_t o) {
+  return __uint_as_float(o ^ (o >> 31 ? 0x80000000u : 0xFFFFFFFFu));
+}
+__device__ __forceinline__ double from_order(uint64_t o) {
+  return __longlong_as_double((long long)(
+      o ^ (o >> 63 ? 0x8000000000000000ull : 0xFFFFFFFFFFFFFFFFull)));
+}
+__device__ __forceinline__ float wave_max(float x) {
+  return from_order(wave_max(to_order(x)));
 }
 template <typename K>
 __device__ __forceinline__ K wave_sum(K x) {
-  x += dpp<kDppPair>(x, x);
-  x += dpp<kDppQuad>(x, x);
-  x += dpp<kDppHalfMirror>(x, x);
-  x += dpp<kDppMirror>(x, x);
+  x += dpp<kDppPair>(K(0), x);
+  x += dpp<kDppQuad>(K(0), x);
+  x += dpp<kDppHalfMirror>(K(0), x);
+  x += dpp<kDppMirror>(K(0), x);
   x += dpp<kDppBcast15, 0xA>(K(0), x);
   x += dpp<kDppBcast31, 0xC>(K(0), x);
   return lane_of(x, 63);

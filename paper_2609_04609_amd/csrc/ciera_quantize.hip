@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(QuantRowsArgs a) {
                        c < a.n_cols ? uint32_t(a.n_cols - c) : 0u);
     }
     bool any;
-    const uint32_t byte = scale_byte(eight_max_bits(octets_amax(o, any)));
+    const uint32_t byte = scale_byte(eight_max(octets_amax(o, any)));
     const float inv = inverse_scale(byte);
     const u32x2 lo = octet_e4m3(any, o[0], inv), hi = octet_e4m3(any, o[1], inv);
     const u32x4 q = {lo[0], lo[1], hi[0], hi[1]};
@@ -189,7 +189,7 @@ __global__ void __launch_bounds__(256)
                             ? uint32_t(a.n_cols - c0) : 0u);
   }
   bool any;
-  uint32_t m = row_max_bits(octets_amax(o, any));
+  uint32_t m = row_max(octets_amax(o, any));
 #pragma unroll
   for (int d = 16; d < 64; d <<= 1) {
     const uint32_t v = __shfl_xor(m, d, 64);

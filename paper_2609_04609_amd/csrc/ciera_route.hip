@@ -9,9 +9,18 @@
 // Which experts are chosen has to be the choice of exact values, not of their
 // fp32 roundings. Where the logits order the values (no bias), they are
 // compared themselves. Else values are computed in fp32, whose error is bounded
-// below (kTolAbs, kTolRel); a token with two neighbours in the order of the
-// choice closer than that is done again in fp64. Some tokens in a thousand are,
-// where scores are spread like a trained router's.
+// below (kTol...); a token with two neighbours in the order of the choice
+// closer than that is done again in fp64. Some tokens in a thousand are, where
+// scores are spread like a trained router's.
+//
+// Vector instructions bound it, not memory: the choice of 8 of 256 with a bias
+// and groups takes 690 a wave. Keys are whole numbers in the floats' order, whose
+// maximum takes the other lane's value within the instruction; float maxima,
+// which quiet NaN first and move lanes apart, took 960. 32768 fp32 tokens of that
+// kind: 43 us (57 with float keys, and unsorted ones); 16384 bf16 tokens, 8 of 64:
+// 8.5 us; 8 of 256 with a bias, no groups: 21 us.
+#include <type_traits>
+
 #include "ciera_expert.h"
 #include "ciera_expert_dev.h"
 
@@ -22,151 +31,269 @@ namespace {
 constexpr uint32_t kWaves = 4;  // tokens per workgroup
 constexpr float kInf = __builtin_inff();
 
-// |fp32 value - exact value| <= kTolAbs + kTolRel |value|. expf is within 1 ulp
-// of its argument's exponential, and its argument (l, or l - max, rounded
-// once: relative 2^-24 of a number x) moves it by |x| 2^-24; s (1 - s) |x| <=
-// 0.28 and p |log p| <= 0.37 bound what that does to a score. The sum of up to
-// 1024 exponentials is off by at most 2^-24 (16 values in a lane, 6 steps)
-// relative to it: 22 half ulps; the division adds 1.5 ulp. Together below (0.37
-// + 1 + 22 / 2 + 1.5) 2^-23 of a score of at most 1, and 2^-24 of the value for
-// the bias's addition.
-constexpr float kTolAbs = 14 * 0x1p-23f;
+// |fp32 value - exact value| <= tol + kTolRel |value|. v_exp_f32 is within 1 ulp
+// (2^-23); its argument x log2(e) is rounded twice (the product and the constant), and
+// x = l - max once, which moves the exponential by at most 1.5 |x| 2^-23 of itself.
+//   sigmoid  s = 1 / (1 + e^-l): the exponential's error counts s (1 - s) <= 1/4 fold,
+//            s (1 - s) |l| <= 0.28, and the sum and the reciprocal are off by 1.5
+//            ulp: (0.25 + 1.5 * 0.28 + 1.5) 2^-23
+//   softmax  of at most the largest score p: |x| p e^x <= 0.37 p; the sum of up
+//            to 1024 exponentials (16 in a lane, 6 steps) by at most 22 half ulps, the
+//            reciprocal and the product by 1.5: (1 + 1.5 * 0.37 + 11 + 1.5) p 2^-23
+// and the bias's addition by half an ulp of the value.
+constexpr float kTolSigmoid = 3 * 0x1p-23f, kTolSoftmax = 15 * 0x1p-23f;
 constexpr float kTolRel = 0x1p-23f;
 
-__device__ __forceinline__ float exp_of(float x) { return expf(x); }
-__device__ __forceinline__ double exp_of(double x) { return exp(x); }
-
-template <typename T, int V>
-__device__ __forceinline__ void load_logits(const RouteArgs &a, uint64_t row,
-                                            uint32_t lane, float (&l)[V]) {
-  const typename T::Raw *p =
-      static_cast<const typename T::Raw *>(a.logits) + row * a.row_stride;
-#pragma unroll
-  for (int j = 0; j < V; ++j) {
-    const uint32_t e = lane * V + j;
-    l[j] = e < a.n_experts ? T::to_float(p[e]) : -kInf;
-  }
+__device__ __forceinline__ float exp_of(float x) {
+  return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f);
 }
+__device__ __forceinline__ double exp_of(double x) { return exp(x); }
+__device__ __forceinline__ float one_over(float x) {
+  return __builtin_amdgcn_rcpf(x);
+}
+__device__ __forceinline__ double one_over(double x) { return 1 / x; }
 
-// Groups that take part, as a mask: the top_groups groups of highest rank
-// among the n_groups groups of `key`. `close`: whether the border between them
-// is within tol. `shared` holds 64 V values of this wave.
-template <typename K, int V>
-__device__ __forceinline__ uint64_t choose_groups(const RouteArgs &a,
-                                                  const K (&key)[V],
-                                                  uint32_t lane, K *shared,
-                                                  float tol_abs, float tol_rel,
-                                                  bool &close) {
-  const uint32_t S = a.n_experts / a.n_groups;
+// V consecutive logits a lane; `vec`: they may be read at once.
+template <typename T, int V>
+__device__ __forceinline__ void load_logits(const typename T::Raw *row,
+                                            uint32_t n_experts, bool vec,
+                                            uint32_t lane, float (&l)[V]) {
+  typename T::Raw raw[V];
+  if (vec) {
+    if (lane * V < n_experts)
+      __builtin_memcpy(raw, __builtin_assume_aligned(row + lane * V,
+                                                     V * T::kBytes < 16
+                                                         ? V * T::kBytes : 16),
+                       V * T::kBytes);
 #pragma unroll
-  for (int j = 0; j < V; ++j) shared[lane * V + j] = key[j];
-  wave_order();
-  K one = -kInf, two = -kInf;
-  if (lane < a.n_groups) {
-    for (uint32_t i = 0; i < S; ++i) {
-      const K v = shared[lane * S + i];
-      const K low = v < one ? v : one;
-      one = larger(one, v);
-      two = larger(two, low);
+    for (int j = 0; j < V; ++j)
+      l[j] = lane * V < n_experts ? T::to_float(raw[j]) : -kInf;
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const uint32_t e = lane * V + j;
+      l[j] = e < n_experts ? T::to_float(row[e]) : -kInf;
     }
   }
-  K rank_by = one;
-  if ((a.flags & CIERA_ROUTE_GROUP_TOP_TWO) && two > -kInf) rank_by = one + two;
-  uint32_t rank = 0;
-  for (uint32_t g = 0; g < a.n_groups; ++g) {
-    const K v = lane_of(rank_by, int(g));
-    rank += (v > rank_by || (v == rank_by && g < lane)) ? 1u : 0u;
-  }
-  const bool kept = lane < a.n_groups && rank < a.top_groups;
-  const K least = -wave_max(kept ? -rank_by : K(-kInf));
-  const K most = wave_max(lane < a.n_groups && !kept ? rank_by : K(-kInf));
-  const K size = larger(larger(least, -least), larger(most, -most));
-  close = most > -kInf && least - most <= 4 * (tol_abs + tol_rel * size);
-  return __ballot(kept);
 }
 
-// One token's choice. Lane s < top_k gets the expert of slot s in `id` (-1:
-// none). Returns false where two values are too close for K.
+// A value's place in the order as a whole number; 0: out of the choice.
+template <typename K>
+using Order = std::conditional_t<sizeof(K) == 4, uint32_t, uint64_t>;
+
+// The two largest of two pairs (one >= two).
+template <typename O>
+__device__ __forceinline__ void merge_two(O &one, O &two, O other_one,
+                                          O other_two) {
+  const O low = one < other_one ? one : other_one;
+  one = larger(one, other_one);
+  two = larger(larger(two, other_two), low);
+}
+
+// Whether neighbours in the order, values of K that are each within tol_abs +
+// tol_rel |value| of what they stand for, could stand in the other order.
+template <typename K>
+__device__ __forceinline__ bool too_close(K above, K below, float parts,
+                                          float tol_abs, float tol_rel) {
+  const K size = larger(larger(above, -above), larger(below, -below));
+  return above - below <= 2 * parts * (tol_abs + tol_rel * size);
+}
+
+// Keep the top_groups groups of highest rank; the keys of others become 0.
+// Returns whether the border between them is closer than K tells apart. Groups
+// of V, 2 V ... 16 V experts are reduced within a row of lanes; other
+// sizes go through `shared`, 64 V keys of this wave, a lane a group.
 template <typename K, int V>
-__device__ __forceinline__ bool choose(const RouteArgs &a, K (&key)[V],
-                                       uint32_t lane, K *shared, float tol_abs,
-                                       float tol_rel, int &id) {
-  if (a.top_groups < a.n_groups) {
-    bool close;
-    const uint64_t groups =
-        choose_groups(a, key, lane, shared, tol_abs, tol_rel, close);
-    if (close && tol_abs > 0) return false;
-    const uint32_t S = a.n_experts / a.n_groups;
+__device__ __forceinline__ bool choose_groups(const RouteArgs &a,
+                                              Order<K> (&key)[V], uint32_t lane,
+                                              Order<K> *shared, float tol_abs,
+                                              float tol_rel) {
+  using O = Order<K>;
+  const uint32_t S = a.n_experts / a.n_groups;
+  const uint32_t lanes = S / V;
+  const bool in_row = S % V == 0 && (lanes & (lanes - 1)) == 0 && lanes <= 16;
+  O one = 0, two = 0;
+  if (in_row) {
+    one = key[0];
+#pragma unroll
+    for (int j = 1; j < V; ++j) merge_two(one, two, key[j], O(0));
+    if (lanes >= 2)
+      merge_two(one, two, dpp_or_zero<kDppPair>(one),
+                dpp_or_zero<kDppPair>(two));
+    if (lanes >= 4)
+      merge_two(one, two, dpp_or_zero<kDppQuad>(one),
+                dpp_or_zero<kDppQuad>(two));
+    if (lanes >= 8)
+      merge_two(one, two, dpp_or_zero<kDppHalfMirror>(one),
+                dpp_or_zero<kDppHalfMirror>(two));
+    if (lanes >= 16)
+      merge_two(one, two, dpp_or_zero<kDppMirror>(one),
+                dpp_or_zero<kDppMirror>(two));
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j) shared[lane * V + j] = key[j];
+    wave_order();
+    if (lane < a.n_groups)
+      for (uint32_t i = 0; i < S; ++i)
+        merge_two(one, two, shared[lane * S + i], O(0));
+  }
+  O rank_by = one;
+  if ((a.flags & CIERA_ROUTE_GROUP_TOP_TWO) && two != 0)
+    rank_by = to_order(from_order(one) + from_order(two));
+  // group g's rank is in lane g * step
+  const uint32_t step = in_row ? lanes : 1, mine = lane / step;
+  uint32_t rank = 0;
+  for (uint32_t g = 0; g < a.n_groups; ++g) {
+    const O v = lane_of(rank_by, int(g * step));
+    rank += (v > rank_by || (v == rank_by && g < mine)) ? 1u : 0u;
+  }
+  const bool kept = mine < a.n_groups && rank < a.top_groups;
+  if (in_row) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) key[j] = kept ? key[j] : O(0);
+  } else {
+    const uint64_t groups = __ballot(kept);
     uint32_t g = lane * V / S, r = lane * V - g * S;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      if (g >= 64 || !((groups >> g) & 1)) key[j] = -kInf;
+      if (g >= 64 || !((groups >> g) & 1)) key[j] = 0;
       if (++r == S) r = 0, ++g;
     }
   }
-  id = -1;
-  K before = kInf;
-  // one round more than slots: the first that is left out must not be close
-  const uint32_t rounds = a.top_k + (tol_abs > 0 ? 1 : 0);
-  for (uint32_t s = 0; s < rounds; ++s) {
-    K best = key[0];
-    int at = 0;
-#pragma unroll
-    for (int j = 1; j < V; ++j)
-      if (key[j] > best) best = key[j], at = j;
-    const K m = wave_max(best);
-    if (m == -kInf) break;
-    if (tol_abs > 0 && s > 0) {
-      const K size = larger(larger(before, -before), larger(m, -m));
-      if (before - m <= 2 * (tol_abs + tol_rel * size)) return false;
-    }
-    before = m;
-    const int first = __builtin_ctzll(__ballot(best == m));
-    const int j = __builtin_amdgcn_readlane(at, first);
-    if (s < a.top_k && lane == s) id = first * V + j;
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (int(lane) == first && i == j) key[i] = -kInf;
-  }
-  return true;
+  if (tol_abs == 0) return false;
+  const O least = ~wave_max(kept ? O(~rank_by) : O(0));
+  const O most = wave_max(mine < a.n_groups && !kept ? rank_by : O(0));
+  // a group's rank has up to two values' errors
+  return most != 0 && too_close(K(from_order(least)), K(from_order(most)), 2,
+                                tol_abs, tol_rel);
 }
 
-// The values that the choice compares, in K.
+// One token's choice. Lane s < top_k gets the expert of slot s in `id` (-1:
+// none). Returns false where two values are too close for K. Up to four keys
+// a lane are sorted first (the lower index ahead among equals), so that a round
+// looks at the lanes' first ones alone; `order` holds their places, two bits each.
 template <typename K, int V>
-__device__ __forceinline__ void values_of(const RouteArgs &a,
-                                          const float (&l)[V], float top,
-                                          uint32_t lane, K (&key)[V]) {
+__device__ __forceinline__ bool choose(const RouteArgs &a, Order<K> (&key)[V],
+                                       uint32_t lane, Order<K> *shared,
+                                       float tol_abs, float tol_rel, int &id) {
+  using O = Order<K>;
+  if (a.top_groups < a.n_groups &&
+      choose_groups<K, V>(a, key, lane, shared, tol_abs, tol_rel))
+    return false;
+  id = -1;
+  constexpr bool kSorted = V <= 4;
+  uint32_t order = 0;
+  if constexpr (kSorted && V > 1) {
+    uint32_t at[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) at[j] = j;
+    const auto in_turn = [&](int x, int y) {
+      const bool swap = key[y] > key[x] || (key[y] == key[x] && at[y] < at[x]);
+      const O k = key[x];
+      const uint32_t i = at[x];
+      key[x] = swap ? key[y] : k;
+      key[y] = swap ? k : key[y];
+      at[x] = swap ? at[y] : i;
+      at[y] = swap ? i : at[y];
+    };
+    if constexpr (V == 2) {
+      in_turn(0, 1);
+    } else {
+      in_turn(0, 1), in_turn(2, 3), in_turn(0, 2), in_turn(1, 3), in_turn(1, 2);
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) order |= at[j] << (2 * j);
+  }
+  // one round more than slots: the first that is left out must not be close
+  const uint32_t rounds = a.top_k + (tol_abs > 0 ? 1 : 0);
+  O chosen = 0;  // lane s: the key of round s
+  bool close = false;
+  for (uint32_t s = 0; s < rounds; ++s) {
+    O best = key[0];
+    uint32_t at = order & 3;
+    if constexpr (!kSorted) {
+      at = 0;
+#pragma unroll
+      for (int j = 1; j < V; ++j)
+        if (key[j] > best) best = key[j], at = j;
+    }
+    const O m = wave_max(best);
+    if (m == 0) break;
+    const uint32_t first = __builtin_ctzll(__ballot(best == m));
+    const uint32_t j = __builtin_amdgcn_readlane(at, int(first));
+    if (lane == s) {
+      chosen = m;
+      id = int(first * V + j);
+    }
+    if (s == 64)  // no lane's round
+      close = too_close(K(from_order(lane_of(chosen, 63))), K(from_order(m)), 1,
+                        tol_abs, tol_rel);
+    const bool taken = lane == first;
+    if constexpr (kSorted) {
+#pragma unroll
+      for (int i = 0; i + 1 < V; ++i) key[i] = taken ? key[i + 1] : key[i];
+      key[V - 1] = taken ? O(0) : key[V - 1];
+      order = taken ? order >> 2 : order;
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (taken && uint32_t(i) == j) key[i] = 0;
+    }
+  }
+  if (lane >= a.top_k) id = -1;
+  if (tol_abs == 0) return true;
+  // a round's value against the one before
+  const O before = __shfl_up(chosen, 1, 64);
+  close = close ||
+          (lane > 0 && chosen != 0 &&
+           too_close(K(from_order(before)), K(from_order(chosen)), 1, tol_abs,
+                     tol_rel));
+  return __ballot(close) == 0;
+}
+
+// The values that the choice compares, computed in K; returns tol.
+template <typename K, int V>
+__device__ __forceinline__ float values_of(const RouteArgs &a,
+                                           const float (&l)[V], float top,
+                                           uint32_t lane, Order<K> (&key)[V]) {
+  float tol = kTolSigmoid;
+  K v[V];
   if (a.flags & CIERA_ROUTE_SIGMOID) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) key[j] = K(1) / (K(1) + exp_of(-K(l[j])));
+    for (int j = 0; j < V; ++j) v[j] = one_over(K(1) + exp_of(-K(l[j])));
   } else {
     K sum = 0;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      key[j] = exp_of(K(l[j]) - K(top));
-      sum += key[j];
+      v[j] = exp_of(K(l[j]) - K(top));
+      sum += v[j];
     }
-    sum = wave_sum(sum);
+    sum = one_over(wave_sum(sum));  // the largest score
+    tol = kTolSoftmax * float(sum);
 #pragma unroll
-    for (int j = 0; j < V; ++j) key[j] /= sum;
+    for (int j = 0; j < V; ++j) v[j] *= sum;
   }
 #pragma unroll
   for (int j = 0; j < V; ++j) {
     const uint32_t e = lane * V + j;
     const float b = a.bias && e < a.n_experts ? a.bias[e] : 0.0f;
     const bool live = l[j] > -kInf && fabsf(b) < kInf;
-    key[j] = live ? key[j] + K(b) : K(-kInf);
+    key[j] = live ? to_order(v[j] + K(b)) : Order<K>(0);
   }
+  return tol;
 }
 
 template <typename T, int V>
-__global__ void __launch_bounds__(64 * kWaves) route_kernel(RouteArgs a) {
-  __shared__ double shared[kWaves][64 * V];
+__global__ void __launch_bounds__(64 * kWaves)
+    route_kernel(RouteArgs a, bool vec) {
+  __shared__ uint64_t shared[kWaves][64 * V];
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const uint32_t token = blockIdx.x * kWaves + wave;
   if (token >= a.n_tokens) return;
   float l[V];
-  load_logits<T, V>(a, token, lane, l);
+  load_logits<T, V>(static_cast<const typename T::Raw *>(a.logits) +
+                        token * a.row_stride,
+                    a.n_experts, vec, lane, l);
   float top = l[0];
   bool fine = l[0] < kInf;  // neither NaN nor +inf
 #pragma unroll
@@ -188,22 +315,21 @@ __global__ void __launch_bounds__(64 * kWaves) route_kernel(RouteArgs a) {
       !a.bias && (all_groups || !(a.flags & CIERA_ROUTE_GROUP_TOP_TWO));
   int id = -1;
   if (top > -kInf) {
-    float key[V];
+    uint32_t key[V];
+    uint32_t *const room = reinterpret_cast<uint32_t *>(shared[wave]);
     bool sure;
     if (by_logit) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) key[j] = l[j];
-      sure = choose(a, key, lane, reinterpret_cast<float *>(shared[wave]),
-                    0.0f, 0.0f, id);
+      for (int j = 0; j < V; ++j) key[j] = l[j] > -kInf ? to_order(l[j]) : 0u;
+      sure = choose<float, V>(a, key, lane, room, 0.0f, 0.0f, id);
     } else {
-      values_of(a, l, top, lane, key);
-      sure = choose(a, key, lane, reinterpret_cast<float *>(shared[wave]),
-                    kTolAbs, kTolRel, id);
+      const float tol = values_of<float, V>(a, l, top, lane, key);
+      sure = choose<float, V>(a, key, lane, room, tol, kTolRel, id);
     }
     if (!sure) {
-      double wide[V];
-      values_of(a, l, top, lane, wide);
-      choose(a, wide, lane, shared[wave], 0.0f, 0.0f, id);
+      uint64_t wide[V];
+      values_of<double, V>(a, l, top, lane, wide);
+      choose<double, V>(a, wide, lane, shared[wave], 0.0f, 0.0f, id);
     }
   }
   // the weights, from the chosen logits
@@ -247,7 +373,7 @@ __global__ void __launch_bounds__(64 * kWaves) route_kernel(RouteArgs a) {
 // row.
 template <typename T, int V>
 __global__ void __launch_bounds__(64 * kWaves)
-    route_backward_kernel(RouteBackArgs a) {
+    route_backward_kernel(RouteBackArgs a, bool vec) {
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const uint32_t token = blockIdx.x * kWaves + wave;
   if (token >= a.n_tokens) return;
@@ -270,13 +396,10 @@ __global__ void __launch_bounds__(64 * kWaves)
   float l[V], spread = 0, top = 0, sum = 1;
   const bool whole = !sigmoid && !normal;
   if (whole) {
+    load_logits<T, V>(row, a.n_experts, vec, lane, l);
     top = -kInf;
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const uint32_t e = lane * V + j;
-      l[j] = e < a.n_experts ? T::to_float(row[e]) : -kInf;
-      top = l[j] > top || l[j] != l[j] ? l[j] : top;
-    }
+    for (int j = 0; j < V; ++j) top = l[j] > top || l[j] != l[j] ? l[j] : top;
     // a NaN stays the maximum's choice of no lane: the sum carries it instead
     top = wave_max(top == top ? top : -kInf);
     sum = 0;
@@ -497,32 +620,42 @@ __global__ void plan_empty_kernel(int32_t *offsets, uint32_t n) {
   for (uint32_t i = threadIdx.x; i < n; i += blockDim.x) offsets[i] = 0;
 }
 
-template <typename T>
-hipError_t route_typed(const RouteArgs &a, hipStream_t s) {
-  const dim3 grid((a.n_tokens + kWaves - 1) / kWaves), block(64 * kWaves);
-  if (a.n_experts <= 64)
-    route_kernel<T, 1><<<grid, block, 0, s>>>(a);
-  else if (a.n_experts <= 128)
-    route_kernel<T, 2><<<grid, block, 0, s>>>(a);
-  else if (a.n_experts <= 256)
-    route_kernel<T, 4><<<grid, block, 0, s>>>(a);
-  else
-    route_kernel<T, 16><<<grid, block, 0, s>>>(a);
-  return hipGetLastError();
+// Whether V values of a row may be read at once at places that are multiples of V.
+bool whole_reads(const void *p, uint64_t stride, uint32_t n, uint32_t V,
+                 uint32_t bytes) {
+  const uint32_t align = V * bytes < 16 ? V * bytes : 16;
+  return n % V == 0 && stride * bytes % align == 0 &&
+         reinterpret_cast<uintptr_t>(p) % align == 0;
 }
 
+template <typename T, int V>
+hipError_t route_wide(const RouteArgs &a, hipStream_t s) {
+  route_kernel<T, V><<<dim3((a.n_tokens + kWaves - 1) / kWaves),
+                       dim3(64 * kWaves), 0, s>>>(
+      a, whole_reads(a.logits, a.row_stride, a.n_experts, V, T::kBytes));
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t route_typed(const RouteArgs &a, hipStream_t s) {
+  return a.n_experts <= 64    ? route_wide<T, 1>(a, s)
+         : a.n_experts <= 128 ? route_wide<T, 2>(a, s)
+         : a.n_experts <= 256 ? route_wide<T, 4>(a, s)
+                              : route_wide<T, 16>(a, s);
+}
+
+template <typename T, int V>
+hipError_t route_back_wide(const RouteBackArgs &a, hipStream_t s) {
+  route_backward_kernel<T, V><<<dim3((a.n_tokens + kWaves - 1) / kWaves),
+                                dim3(64 * kWaves), 0, s>>>(
+      a, whole_reads(a.logits, a.row_stride, a.n_experts, V, T::kBytes));
+  return hipGetLastError();
+}
 template <typename T>
 hipError_t route_back_typed(const RouteBackArgs &a, hipStream_t s) {
-  const dim3 grid((a.n_tokens + kWaves - 1) / kWaves), block(64 * kWaves);
-  if (a.n_experts <= 64)
-    route_backward_kernel<T, 1><<<grid, block, 0, s>>>(a);
-  else if (a.n_experts <= 128)
-    route_backward_kernel<T, 2><<<grid, block, 0, s>>>(a);
-  else if (a.n_experts <= 256)
-    route_backward_kernel<T, 4><<<grid, block, 0, s>>>(a);
-  else
-    route_backward_kernel<T, 16><<<grid, block, 0, s>>>(a);
-  return hipGetLastError();
+  return a.n_experts <= 64    ? route_back_wide<T, 1>(a, s)
+         : a.n_experts <= 128 ? route_back_wide<T, 2>(a, s)
+         : a.n_experts <= 256 ? route_back_wide<T, 4>(a, s)
+                              : route_back_wide<T, 16>(a, s);
 }
 
 }  // namespace
