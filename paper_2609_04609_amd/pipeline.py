@@ -22,7 +22,9 @@ of its encode would meet a bad header or stale bytes and leave wrong values,
 so the schedule's event waits carry the data, not only the timing. The
 Allgather itself is a stand-in: a one-thread spin kernel (torch.cuda._sleep)
 lasting the alpha-beta time alpha + (R-1) x / bw of the encoded payload x.
-Compute_i is a bf16 linear layer over the decoded weights. Encode, cache
+Compute_i is a bf16 linear layer over the decoded weights or, with `experts`,
+the forward and backward pass of a layer of experts whose weights they are (its
+8-bit copies of the weights are made anew from every decode). Encode, cache
 update and decode are the library's kernels through the C ABI; nothing here
 computes codec data.
 """
@@ -32,6 +34,7 @@ import numpy as np
 import torch
 
 from . import ciera
+from .experts import ExpertLayer
 
 
 def calibrate_sleep(stream, cycles=2_000_000, reps=5):
@@ -51,10 +54,13 @@ def calibrate_sleep(stream, cycles=2_000_000, reps=5):
 
 class OverlapPipeline:
     """L layer groups sharing one set of shards (the codec work per layer is
-    the same), each with its own receiver caches, sender cache and output."""
+    the same), each with its own receiver caches, sender cache and output.
+    ``experts``: None, or (experts, chosen per token, input width) of the
+    layers of experts that the decoded weights are; their output width is what
+    the weights leave."""
 
     def __init__(self, setup, layers, link_bw_Bps, alpha_s=10e-6,
-                 tokens=256, caches_hold_w2=False):
+                 tokens=256, caches_hold_w2=False, experts=None):
         S = setup
         self.S, self.L = S, layers
         self.n, self.R, self.B = S.n, S.R, S.B
@@ -70,14 +76,33 @@ class OverlapPipeline:
         # 0's slot [0, total_0) is rewritten by the sender every step
         self.gath = [(S.gA.clone(), S.gB.clone()) for _ in range(layers)]
         self.slot0 = (int(S.totA[0]), int(S.totB[0]))
-        # compute stand-in: x [tokens, 4096] times the decoded layer viewed as
-        # [R n / 4096, 4096] bf16 weights
-        self.k = 4096
-        self.rows = (self.R * self.n) // self.k
-        self.act = torch.randn(tokens, self.k, device=dev,
-                               dtype=torch.bfloat16)
-        self.y = [torch.empty(tokens, self.rows, device=dev,
-                              dtype=torch.bfloat16) for _ in range(layers)]
+        if experts is None:
+            # compute stand-in: x [tokens, 4096] times the decoded layer viewed
+            # as [R n / 4096, 4096] bf16 weights
+            self.k = 4096
+            self.rows = (self.R * self.n) // self.k
+            self.act = torch.randn(tokens, self.k, device=dev,
+                                   dtype=torch.bfloat16)
+            self.y = [torch.empty(tokens, self.rows, device=dev,
+                                  dtype=torch.bfloat16)
+                      for _ in range(layers)]
+        else:
+            n_experts, top_k, self.k = experts
+            self.rows, rest = divmod(self.R * self.n, n_experts * self.k)
+            if rest:
+                raise ValueError(f"{self.R * self.n} weights are not "
+                                 f"{n_experts} experts of {self.k} columns")
+            self.act = torch.randn(tokens, self.k, device=dev,
+                                   dtype=torch.bfloat16)
+            self.d_y = torch.randn(tokens, self.rows, device=dev,
+                                   dtype=torch.bfloat16)
+            self.logits = torch.randn(tokens, n_experts, device=dev,
+                                      dtype=torch.bfloat16)
+            self.experts = [ExpertLayer(tokens, top_k, n_experts, self.rows,
+                                        self.k, device=dev, normalize=True)
+                            for _ in range(layers)]
+            self.y = [e.out for e in self.experts]
+        self.with_experts = experts is not None
         self.s_send = torch.cuda.Stream(device=dev)
         self.s_link = torch.cuda.Stream(device=dev)
         self.s_recv = torch.cuda.Stream(device=dev)
@@ -122,6 +147,18 @@ class OverlapPipeline:
         self._poison(i, side)
         return self._encode(i, w_in, side)
 
+    def _compute(self, i):
+        """Layer i's compute over its decoded weights, on the current
+        stream."""
+        w = self.outs[i].view(torch.bfloat16)
+        if self.with_experts:
+            e = self.experts[i]
+            e.load(w.view(e.E, e.N, e.C))
+            e.forward(self.act, self.logits)
+            e.backward(self.d_y, self.act, self.logits)
+        else:
+            torch.mm(self.act, w.view(self.rows, self.k).t(), out=self.y[i])
+
     def _layer(self, i, w_in, side, off, link_us, st_send, st_link, st_recv,
                st_comp, ev=None):
         n, B = self.n, self.B
@@ -145,8 +182,7 @@ class OverlapPipeline:
         with torch.cuda.stream(st_comp):
             if ev is not None:
                 st_comp.wait_event(ev["dec"][i])
-            w = self.outs[i].view(torch.bfloat16).view(self.rows, self.k)
-            torch.mm(self.act, w.t(), out=self.y[i])
+            self._compute(i)
 
     def step(self, overlapped):
         """One iteration over all L layers; returns the wall time in us
@@ -218,8 +254,7 @@ class OverlapPipeline:
             ciera.decode_gathered_t(g, off, self.n, self.B, self.outs[0],
                                     self.caches[0], self.ws_dec[0])
             ev[3].record(main)
-            w = self.outs[0].view(torch.bfloat16).view(self.rows, self.k)
-            torch.mm(self.act, w.t(), out=self.y[0])
+            self._compute(0)
             ev[4].record(main)
             torch.cuda.synchronize()
             for k, name in enumerate(names):
