@@ -43,8 +43,8 @@ struct RouteBackArgs {
   uint64_t d_row_stride;
 };
 
-// Plan: pairs that one workgroup sorts, and its counts in the workspace (one
-// word per expert and tile, expert by expert).
+// Plan: pairs that one workgroup sorts, and its counts in the workspace: one
+// word per expert and tile, expert by expert, then one per expert.
 constexpr uint32_t kPlanTile = 2048;
 struct PlanArgs {
   const int32_t *ids;

@@ -102,7 +102,7 @@ uint64_t ciera_plan_workspace_bytes(uint64_t n_tokens, uint32_t top_k,
       top_k > CIERA_MAX_TOP_K || n_tokens >= kMost || n_tokens * top_k >= kMost)
     return 0;
   const uint64_t tiles = plan_tiles(n_tokens * top_k);
-  return ((tiles * n_experts + 1) * 4 + 255) & ~uint64_t(255);
+  return ((tiles + 1) * n_experts * 4 + 255) & ~uint64_t(255);
 }
 
 int ciera_route_plan(const int32_t *expert_ids, uint64_t n_tokens,

@@ -128,9 +128,11 @@ __device__ __forceinline__ float times(float x, float inv) {
 
 // ------------------------------------------------------ across a wave ----
 // DPP controls: the other lane of a pair or of a pair of pairs, the mirrored
-// lane of 8 or 16, and lane 15 (31) to the row (the half) behind it.
+// lane of 8 or 16, lane 15 (31) to the row (the half) behind it, and within a
+// row the lane n below (kDppUp + n).
 constexpr int kDppPair = 0xB1, kDppQuad = 0x4E, kDppHalfMirror = 0x141,
-              kDppMirror = 0x140, kDppBcast15 = 0x142, kDppBcast31 = 0x143;
+              kDppMirror = 0x140, kDppBcast15 = 0x142, kDppBcast31 = 0x143,
+              kDppUp = 0x110;
 
 // x of the lane that CTRL names; `old` where there is none
 template <int CTRL, int ROWS = 0xF>
@@ -159,10 +161,10 @@ __device__ __forceinline__ double lane_of(double x, int lane) {
 
 // Whole numbers of 32 and 64 bits. 0, or a lane without a source, is the least:
 // a maximum takes the other lane's value in one instruction.
-template <int CTRL>
+template <int CTRL, int ROWS = 0xF>
 __device__ __forceinline__ uint32_t dpp_or_zero(uint32_t x) {
   return uint32_t(
-      __builtin_amdgcn_update_dpp(0, int(x), CTRL, 0xF, 0xF, false));
+      __builtin_amdgcn_update_dpp(0, int(x), CTRL, ROWS, 0xF, false));
 }
 template <int CTRL>
 __device__ __forceinline__ uint64_t dpp_or_zero(uint64_t x) {
@@ -238,14 +240,14 @@ __device__ __forceinline__ void wave_order() {
 }
 
 // sum of x over the lanes below this one, and over the wave
-__device__ __forceinline__ uint32_t wave_prefix(uint32_t x, uint32_t lane,
-                                                uint32_t &total) {
+__device__ __forceinline__ uint32_t wave_prefix(uint32_t x, uint32_t &total) {
   uint32_t s = x;
-#pragma unroll
-  for (uint32_t d = 1; d < 64; d <<= 1) {
-    const uint32_t y = __shfl_up(s, d, 64);
-    if (lane >= d) s += y;
-  }
+  s += dpp_or_zero<kDppUp + 1>(s);
+  s += dpp_or_zero<kDppUp + 2>(s);
+  s += dpp_or_zero<kDppUp + 4>(s);
+  s += dpp_or_zero<kDppUp + 8>(s);
+  s += dpp_or_zero<kDppBcast15, 0xA>(s);
+  s += dpp_or_zero<kDppBcast31, 0xC>(s);
   total = __builtin_amdgcn_readlane(s, 63);
   return s - x;
 }
@@ -281,7 +283,7 @@ __device__ __forceinline__ ExpertTile find_tile(const int32_t *offsets,
     }
     const uint32_t tiles = (hi - lo + (1u << log2_tile) - 1) >> log2_tile;
     uint32_t total;
-    const uint32_t start = before + wave_prefix(tiles, lane, total);
+    const uint32_t start = before + wave_prefix(tiles, total);
     const uint64_t here = __ballot(tile >= start && tile < start + tiles);
     if (here) {
       const int l = __builtin_ctzll(here);

@@ -562,7 +562,7 @@ __device__ __forceinline__ void sum_experts(Sums &s, const int32_t *offsets,
     uint32_t total;
     const uint32_t start =
         before +
-        wave_prefix((hi - lo + (1u << log2_unit) - 1) >> log2_unit, lane, total);
+        wave_prefix((hi - lo + (1u << log2_unit) - 1) >> log2_unit, total);
     before += total;
     if (e < n_experts) {
       s.before[e] = start;
@@ -1024,7 +1024,7 @@ __device__ __forceinline__ void blocks_of_expert(const int32_t *offsets,
     sum += hi > lo ? (hi - lo + 127) / 128 : 0;
   }
   uint32_t total;
-  wave_prefix(sum, lane, total);
+  wave_prefix(sum, total);
   start = total;
   const uint32_t lo = offset_of(offsets, expert, ~0u);
   const uint32_t hi = offset_of(offsets, expert + 1, ~0u);

@@ -448,11 +448,12 @@ __global__ void __launch_bounds__(64 * kWaves)
 }
 
 // ----------------------------------------------------------------- plan ----
-// A stable counting sort. Tiles of kPlanTile pairs are counted, the counts
-// scanned expert by expert, and every tile places its pairs: each wave takes a
-// run of the tile, and among 64 pairs those of the same expert are found by
-// ballots over the bits of the id. Up to one tile is sorted by one workgroup in
-// one launch. Nothing depends on the order in which waves run.
+// A stable counting sort. Tiles of kPlanTile pairs are counted, every expert's
+// counts scanned by a wave, and every tile places its pairs behind the experts
+// before (it scans their totals itself): each wave takes a run of the tile, and
+// among 64 pairs those of the same expert are found by ballots over the bits of
+// the id. Up to one tile is sorted by one workgroup in one launch. Nothing depends on
+// the order in which waves run.
 constexpr uint32_t kPlanThreads = 512;
 constexpr uint32_t kPlanWaves = kPlanThreads / 64;
 constexpr uint32_t kPlanRun = kPlanTile / kPlanWaves;  // pairs per wave
@@ -488,38 +489,30 @@ __global__ void __launch_bounds__(kPlanThreads)
     a.counts[uint64_t(e) * tiles + blockIdx.x] = count[e];
 }
 
-// The counts' running sum in place: where each tile's first row of each expert
-// is; counts[n_experts * tiles] gets the total.
-__global__ void __launch_bounds__(1024)
+// A wave an expert: its counts' running sum in place, where the tile's first row
+// is among the expert's, and its total behind all experts' counts.
+__global__ void __launch_bounds__(256)
     plan_scan_kernel(PlanArgs a, uint32_t tiles) {
-  __shared__ uint32_t wave_total[16];
-  const uint32_t n = a.n_experts * tiles;
-  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr uint32_t kAtOnce = 8;
+  const uint32_t lane = threadIdx.x & 63;
+  const uint32_t e = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (e >= a.n_experts) return;
+  uint32_t *const row = a.counts + uint64_t(e) * tiles;
   uint32_t base = 0;
-  for (uint32_t from = 0; from < n; from += 1024) {
-    const uint32_t i = from + threadIdx.x;
-    const uint32_t c = i < n ? a.counts[i] : 0;
-    uint32_t total;
-    uint32_t before = wave_prefix(c, lane, total);
-    if (lane == 0) wave_total[wave] = total;
-    __syncthreads();
-    uint32_t all = 0;
+  for (uint32_t from = lane; from - lane < tiles; from += 64 * kAtOnce) {
+    uint32_t c[kAtOnce];
 #pragma unroll
-    for (uint32_t w = 0; w < 16; ++w) {
-      if (w < wave) before += wave_total[w];
-      all += wave_total[w];
+    for (uint32_t j = 0; j < kAtOnce; ++j)
+      c[j] = from + 64 * j < tiles ? row[from + 64 * j] : 0;
+#pragma unroll
+    for (uint32_t j = 0; j < kAtOnce; ++j) {
+      uint32_t total;
+      const uint32_t before = wave_prefix(c[j], total);
+      if (from + 64 * j < tiles) row[from + 64 * j] = base + before;
+      base += total;
     }
-    __syncthreads();
-    if (i < n) {
-      a.counts[i] = base + before;
-      if (i % tiles == 0) a.offsets[i / tiles] = int32_t(base + before);
-    }
-    base += all;
   }
-  if (threadIdx.x == 0) {
-    a.counts[n] = base;
-    a.offsets[a.n_experts] = int32_t(base);
-  }
+  if (lane == 0) a.counts[uint64_t(a.n_experts) * tiles + e] = base;
 }
 
 template <bool ONE>
@@ -527,7 +520,7 @@ __global__ void __launch_bounds__(kPlanThreads)
     plan_place_kernel(PlanArgs a, uint32_t tiles, uint32_t bits) {
   // where the next pair of each expert goes, for every wave of the tile
   __shared__ uint32_t next[kPlanWaves][CIERA_MAX_EXPERTS];
-  __shared__ uint32_t part[kPlanWaves + 1];
+  __shared__ uint32_t part[kPlanWaves];
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for (uint32_t e = threadIdx.x; e < a.n_experts; e += kPlanThreads)
 #pragma unroll
@@ -544,59 +537,51 @@ __global__ void __launch_bounds__(kPlanThreads)
     if (mine[r] < a.n_experts) atomicAdd(&next[wave][mine[r]], 1u);
   }
   __syncthreads();
-  uint32_t total;
-  if constexpr (ONE) {
-    // the workgroup's own scan over experts: each thread's experts are
-    // consecutive
-    constexpr uint32_t kPer = CIERA_MAX_EXPERTS / kPlanThreads;
-    uint32_t c[kPer], sum = 0;
+  // Every workgroup scans the experts' totals; each thread's are consecutive.
+  constexpr uint32_t kPer = CIERA_MAX_EXPERTS / kPlanThreads;
+  uint32_t c[kPer], sum = 0;
 #pragma unroll
-    for (uint32_t j = 0; j < kPer; ++j) {
-      const uint32_t e = threadIdx.x * kPer + j;
-      c[j] = 0;
-      if (e < a.n_experts)
+  for (uint32_t j = 0; j < kPer; ++j) {
+    const uint32_t e = threadIdx.x * kPer + j;
+    c[j] = 0;
+    if (e < a.n_experts) {
+      if constexpr (ONE) {
 #pragma unroll
         for (uint32_t w = 0; w < kPlanWaves; ++w) c[j] += next[w][e];
-      sum += c[j];
-    }
-    uint32_t wave_all;
-    uint32_t before = wave_prefix(sum, lane, wave_all);
-    if (lane == 0) part[wave] = wave_all;
-    __syncthreads();
-    total = 0;
-#pragma unroll
-    for (uint32_t w = 0; w < kPlanWaves; ++w) {
-      if (w < wave) before += part[w];
-      total += part[w];
-    }
-#pragma unroll
-    for (uint32_t j = 0; j < kPer; ++j) {
-      const uint32_t e = threadIdx.x * kPer + j;
-      if (e < a.n_experts) {
-        a.offsets[e] = int32_t(before);
-        uint32_t at = before;
-#pragma unroll
-        for (uint32_t w = 0; w < kPlanWaves; ++w) {
-          const uint32_t n = next[w][e];
-          next[w][e] = at;
-          at += n;
-        }
-        before += c[j];
+      } else {
+        c[j] = a.counts[uint64_t(a.n_experts) * tiles + e];
       }
     }
-    if (threadIdx.x == 0) a.offsets[a.n_experts] = int32_t(total);
-  } else {
-    total = a.counts[uint64_t(a.n_experts) * tiles];
-    for (uint32_t e = threadIdx.x; e < a.n_experts; e += kPlanThreads) {
-      uint32_t at = a.counts[uint64_t(e) * tiles + blockIdx.x];
+    sum += c[j];
+  }
+  uint32_t wave_all;
+  uint32_t before = wave_prefix(sum, wave_all);
+  if (lane == 0) part[wave] = wave_all;
+  __syncthreads();
+  uint32_t total = 0;
+#pragma unroll
+  for (uint32_t w = 0; w < kPlanWaves; ++w) {
+    if (w < wave) before += part[w];
+    total += part[w];
+  }
+#pragma unroll
+  for (uint32_t j = 0; j < kPer; ++j) {
+    const uint32_t e = threadIdx.x * kPer + j;
+    if (e < a.n_experts) {
+      if (blockIdx.x == 0) a.offsets[e] = int32_t(before);
+      uint32_t at = before;
+      if constexpr (!ONE) at += a.counts[uint64_t(e) * tiles + blockIdx.x];
 #pragma unroll
       for (uint32_t w = 0; w < kPlanWaves; ++w) {
         const uint32_t n = next[w][e];
         next[w][e] = at;
         at += n;
       }
+      before += c[j];
     }
   }
+  if (blockIdx.x == 0 && threadIdx.x == 0)
+    a.offsets[a.n_experts] = int32_t(total);
   __syncthreads();
 #pragma unroll
   for (uint32_t r = 0; r < kPlanRun / 64; ++r) {
@@ -685,7 +670,7 @@ hipError_t launch_route_plan(const PlanArgs &a, hipStream_t s) {
     return hipGetLastError();
   }
   plan_count_kernel<<<tiles, kPlanThreads, 0, s>>>(a, tiles);
-  plan_scan_kernel<<<1, 1024, 0, s>>>(a, tiles);
+  plan_scan_kernel<<<(a.n_experts + 3) / 4, 256, 0, s>>>(a, tiles);
   plan_place_kernel<false><<<tiles, kPlanThreads, 0, s>>>(a, tiles, bits);
   return hipGetLastError();
 }
