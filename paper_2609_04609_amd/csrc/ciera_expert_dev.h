@@ -221,11 +221,15 @@ __device__ __forceinline__ float wave_max(float x) {
   return from_order(wave_max(to_order(x)));
 }
 template <typename K>
-__device__ __forceinline__ K wave_sum(K x) {
+__device__ __forceinline__ K row_sum(K x) {  // in every lane of the row
   x += dpp<kDppPair>(K(0), x);
   x += dpp<kDppQuad>(K(0), x);
   x += dpp<kDppHalfMirror>(K(0), x);
-  x += dpp<kDppMirror>(K(0), x);
+  return x + dpp<kDppMirror>(K(0), x);
+}
+template <typename K>
+__device__ __forceinline__ K wave_sum(K x) {
+  x = row_sum(x);
   x += dpp<kDppBcast15, 0xA>(K(0), x);
   x += dpp<kDppBcast31, 0xC>(K(0), x);
   return lane_of(x, 63);

@@ -1,10 +1,10 @@
 // Routing to experts for CDNA4 (gfx950): the choice of experts with its
 // weights, their gradient, and the plan that sorts (token, slot) by expert.
 //
-// A wave holds a token: lane i has the V consecutive experts from V i on, so
-// that the lowest lane of a ballot is the lowest expert among equals, and a
-// token's logits are one coalesced read. The choice is top_k rounds of a
-// maximum over the wave (DPP, no LDS) and one ballot.
+// A team of lanes holds a token, a wave or, for many tokens, 16 lanes: lane i
+// has the V consecutive experts from V i on, so that the lowest lane of a ballot
+// is the lowest expert among equals, and a token's logits are one coalesced read. The
+// choice is top_k rounds of a maximum over the team (DPP, no LDS) and one ballot.
 //
 // Which experts are chosen has to be the choice of exact values, not of their
 // fp32 roundings. Where the logits order the values (no bias), they are
@@ -13,12 +13,12 @@
 // closer than that is done again in fp64. Some tokens in a thousand are, where
 // scores are spread like a trained router's.
 //
-// Vector instructions bound it, not memory: the choice of 8 of 256 with a bias
-// and groups takes 690 a wave. Keys are whole numbers in the floats' order, whose
-// maximum takes the other lane's value within the instruction; float maxima,
-// which quiet NaN first and move lanes apart, took 960. 32768 fp32 tokens of that
-// kind: 43 us (57 with float keys, and unsorted ones); 16384 bf16 tokens, 8 of 64:
-// 8.5 us; 8 of 256 with a bias, no groups: 21 us.
+// Vector instructions bound it, not memory. Keys are whole numbers in the floats'
+// order, whose maximum takes the other lane's value within the instruction (float
+// maxima quiet NaN first and move lanes apart), and what a round costs a wave, a
+// wave of four teams pays once for four tokens. 32768 fp32 tokens, 8 of 256 with a
+// bias and groups: 23 us (37 a wave per token, 57 with float keys; their bytes
+// take 8); bf16 tokens, 8 of 256: 12.7 us, 8 of 64: 6.8 us.
 #include <type_traits>
 
 #include "ciera_expert.h"
@@ -28,7 +28,12 @@ namespace ciera {
 
 namespace {
 
-constexpr uint32_t kWaves = 4;  // tokens per workgroup
+constexpr uint32_t kWaves = 4;  // of a workgroup
+// Tokens from which four share a wave, that the card's 1024 SIMDs still have a
+// wave each. 8 of 256 with a bias and groups, us a wave per token and per four:
+// 1024 tokens 8.7 and 10.1, 4096 10.6 and 10.3, 32768 37 and 23; 8 of 64: 3.3 and
+// 3.5, 4.0 and 3.7, 13.4 and 6.8.
+constexpr uint32_t kRowTokens = 4096;
 constexpr float kInf = __builtin_inff();
 
 // |fp32 value - exact value| <= tol + kTolRel |value|. v_exp_f32 is within 1 ulp
@@ -55,9 +60,10 @@ __device__ __forceinline__ double one_over(double x) { return 1 / x; }
 
 // V consecutive logits a lane; `vec`: they may be read at once.
 template <typename T, int V>
-__device__ __forceinline__ void load_logits(const typename T::Raw *row,
+__device__ __forceinline__ void load_logits(const void *values,
                                             uint32_t n_experts, bool vec,
                                             uint32_t lane, float (&l)[V]) {
+  const auto *row = static_cast<const typename T::Raw *>(values);
   typename T::Raw raw[V];
   if (vec) {
     if (lane * V < n_experts)
@@ -81,6 +87,13 @@ __device__ __forceinline__ void load_logits(const typename T::Raw *row,
 template <typename K>
 using Order = std::conditional_t<sizeof(K) == 4, uint32_t, uint64_t>;
 
+// c ? a : b of values. Written out, the choice between two elements of an array
+// is one between their addresses, and the array is searched.
+template <typename O>
+__device__ __forceinline__ O either(bool c, O a, O b) {
+  return c ? a : b;
+}
+
 // The two largest of two pairs (one >= two).
 template <typename O>
 __device__ __forceinline__ void merge_two(O &one, O &two, O other_one,
@@ -99,19 +112,57 @@ __device__ __forceinline__ bool too_close(K above, K below, float parts,
   return above - below <= 2 * parts * (tol_abs + tol_rel * size);
 }
 
+// A team of L lanes, 64 or 16 (a row), holds a token; `lane` counts in the team.
+template <int L, typename O>
+__device__ __forceinline__ O team_max(O x) {
+  if constexpr (L == 64)
+    return wave_max(x);
+  else
+    return row_max(x);
+}
+template <int L, typename K>
+__device__ __forceinline__ K team_sum(K x) {
+  if constexpr (L == 64)
+    return wave_sum(x);
+  else
+    return row_sum(x);
+}
+// the team's lanes with p
+template <int L>
+__device__ __forceinline__ auto team_bits(bool p) {
+  if constexpr (L == 64)
+    return uint64_t(__ballot(p));
+  else
+    return uint32_t(__ballot(p) >> (threadIdx.x & 48)) & 0xFFFFu;
+}
+// x of the team's lane i
+template <int L, typename O>
+__device__ __forceinline__ O team_lane(O x, uint32_t i) {
+  if constexpr (L == 64)
+    return lane_of(x, int(i));
+  else
+    return __shfl(x, int(i), L);
+}
+
+// Whether groups of S experts are whole lanes of a row, 1, 2, 4 ... 16 of them.
+__host__ __device__ inline bool groups_in_row(uint32_t S, uint32_t V) {
+  const uint32_t lanes = S / V;
+  return S % V == 0 && (lanes & (lanes - 1)) == 0 && lanes <= 16;
+}
+
 // Keep the top_groups groups of highest rank; the keys of others become 0.
 // Returns whether the border between them is closer than K tells apart. Groups
-// of V, 2 V ... 16 V experts are reduced within a row of lanes; other
-// sizes go through `shared`, 64 V keys of this wave, a lane a group.
-template <typename K, int V>
+// in a row are reduced there; others, for teams of 64, go through `shared`, 64 V
+// keys of this wave, a lane a group.
+template <typename K, int V, int L>
 __device__ __forceinline__ bool choose_groups(const RouteArgs &a,
                                               Order<K> (&key)[V], uint32_t lane,
-                                              Order<K> *shared, float tol_abs,
-                                              float tol_rel) {
+                                              Order<K> *shared, bool inexact,
+                                              float tol_abs, float tol_rel) {
   using O = Order<K>;
   const uint32_t S = a.n_experts / a.n_groups;
   const uint32_t lanes = S / V;
-  const bool in_row = S % V == 0 && (lanes & (lanes - 1)) == 0 && lanes <= 16;
+  const bool in_row = L == 16 || groups_in_row(S, V);
   O one = 0, two = 0;
   if (in_row) {
     one = key[0];
@@ -144,13 +195,13 @@ __device__ __forceinline__ bool choose_groups(const RouteArgs &a,
   const uint32_t step = in_row ? lanes : 1, mine = lane / step;
   uint32_t rank = 0;
   for (uint32_t g = 0; g < a.n_groups; ++g) {
-    const O v = lane_of(rank_by, int(g * step));
-    rank += (v > rank_by || (v == rank_by && g < mine)) ? 1u : 0u;
+    const O v = team_lane<L>(rank_by, g * step);
+    rank += uint32_t((v > rank_by) | ((v == rank_by) & (g < mine)));
   }
   const bool kept = mine < a.n_groups && rank < a.top_groups;
   if (in_row) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) key[j] = kept ? key[j] : O(0);
+    for (int j = 0; j < V; ++j) key[j] = either(kept, key[j], O(0));
   } else {
     const uint64_t groups = __ballot(kept);
     uint32_t g = lane * V / S, r = lane * V - g * S;
@@ -160,102 +211,105 @@ __device__ __forceinline__ bool choose_groups(const RouteArgs &a,
       if (++r == S) r = 0, ++g;
     }
   }
-  if (tol_abs == 0) return false;
-  const O least = ~wave_max(kept ? O(~rank_by) : O(0));
-  const O most = wave_max(mine < a.n_groups && !kept ? rank_by : O(0));
+  if (!inexact) return false;
+  const O least = ~team_max<L>(kept ? O(~rank_by) : O(0));
+  const O most = team_max<L>(mine < a.n_groups && !kept ? rank_by : O(0));
   // a group's rank has up to two values' errors
   return most != 0 && too_close(K(from_order(least)), K(from_order(most)), 2,
                                 tol_abs, tol_rel);
 }
 
 // One token's choice. Lane s < top_k gets the expert of slot s in `id` (-1:
-// none). Returns false where two values are too close for K. Up to four keys
-// a lane are sorted first (the lower index ahead among equals), so that a round
-// looks at the lanes' first ones alone; `order` holds their places, two bits each.
-template <typename K, int V>
+// none). Returns false where two values, if inexact, are too close. A lane's keys are
+// sorted first in runs of up to four (the lower index ahead among equals), so that
+// a round looks at the runs' first ones alone; `order` holds the indexes of a
+// run, a byte each. `slot`: L words of this team.
+template <typename K, int V, int L>
 __device__ __forceinline__ bool choose(const RouteArgs &a, Order<K> (&key)[V],
                                        uint32_t lane, Order<K> *shared,
+                                       uint32_t *slot, bool inexact,
                                        float tol_abs, float tol_rel, int &id) {
   using O = Order<K>;
-  if (a.top_groups < a.n_groups &&
-      choose_groups<K, V>(a, key, lane, shared, tol_abs, tol_rel))
-    return false;
-  id = -1;
-  constexpr bool kSorted = V <= 4;
-  uint32_t order = 0;
-  if constexpr (kSorted && V > 1) {
-    uint32_t at[V];
+  bool close = false;
+  if (a.top_groups < a.n_groups)
+    close = choose_groups<K, V, L>(a, key, lane, shared, inexact, tol_abs,
+                                      tol_rel);
+  constexpr int kRun = V < 4 ? V : 4, kRuns = V / kRun;
+  uint32_t order[kRuns];
 #pragma unroll
-    for (int j = 0; j < V; ++j) at[j] = j;
-    const auto in_turn = [&](int x, int y) {
-      const bool swap = key[y] > key[x] || (key[y] == key[x] && at[y] < at[x]);
-      const O k = key[x];
-      const uint32_t i = at[x];
-      key[x] = swap ? key[y] : k;
-      key[y] = swap ? k : key[y];
-      at[x] = swap ? at[y] : i;
-      at[y] = swap ? i : at[y];
+  for (int r = 0; r < kRuns; ++r) {
+    uint32_t at[kRun];
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) at[j] = r * kRun + j;
+    const auto in_turn = [&](int x) {
+      const O k = key[r * kRun + x], n = key[r * kRun + x + 1];
+      const uint32_t i = at[x], m = at[x + 1];
+      const bool swap = n > k;
+      key[r * kRun + x] = either(swap, n, k);
+      key[r * kRun + x + 1] = either(swap, k, n);
+      at[x] = either(swap, m, i);
+      at[x + 1] = either(swap, i, m);
     };
-    if constexpr (V == 2) {
-      in_turn(0, 1);
-    } else {
-      in_turn(0, 1), in_turn(2, 3), in_turn(0, 2), in_turn(1, 3), in_turn(1, 2);
+    // neighbours alone change places, so equals keep their order
+    if constexpr (kRun == 2) {
+      in_turn(0);
+    } else if constexpr (kRun == 4) {
+      in_turn(0), in_turn(2), in_turn(1), in_turn(0), in_turn(2), in_turn(1);
     }
+    order[r] = 0;
 #pragma unroll
-    for (int j = 0; j < V; ++j) order |= at[j] << (2 * j);
+    for (int j = 0; j < kRun; ++j) order[r] |= at[j] << (8 * j);
   }
   // one round more than slots: the first that is left out must not be close
-  const uint32_t rounds = a.top_k + (tol_abs > 0 ? 1 : 0);
-  O chosen = 0;  // lane s: the key of round s
-  bool close = false;
+  const uint32_t rounds = a.top_k + (inexact ? 1 : 0);
+  O chosen = 0, last = 0;  // lane s: the key of round s; the last round's
   for (uint32_t s = 0; s < rounds; ++s) {
     O best = key[0];
-    uint32_t at = order & 3;
-    if constexpr (!kSorted) {
-      at = 0;
+    uint32_t at = order[0], from = 0;
 #pragma unroll
-      for (int j = 1; j < V; ++j)
-        if (key[j] > best) best = key[j], at = j;
+    for (int r = 1; r < kRuns; ++r) {
+      const bool more = key[r * kRun] > best;
+      best = either(more, key[r * kRun], best);
+      at = either(more, order[r], at);
+      from = either(more, uint32_t(r), from);
     }
-    const O m = wave_max(best);
-    if (m == 0) break;
-    const uint32_t first = __builtin_ctzll(__ballot(best == m));
-    const uint32_t j = __builtin_amdgcn_readlane(at, int(first));
-    if (lane == s) {
-      chosen = m;
-      id = int(first * V + j);
-    }
-    if (s == 64)  // no lane's round
-      close = too_close(K(from_order(lane_of(chosen, 63))), K(from_order(m)), 1,
-                        tol_abs, tol_rel);
-    const bool taken = lane == first;
-    if constexpr (kSorted) {
+    last = team_max<L>(best);
+    if (__ballot(last != 0) == 0) break;
+    const auto who = team_bits<L>(best == last);
+    const bool first = (who & (~who + 1)) == decltype(who)(1) << lane;
+    const bool taken = (last != 0) & first;
+    if (taken & (s < a.top_k)) slot[s] = lane * V + (at & 0xFF);
+    chosen = either(lane == s, last, chosen);
 #pragma unroll
-      for (int i = 0; i + 1 < V; ++i) key[i] = taken ? key[i + 1] : key[i];
-      key[V - 1] = taken ? O(0) : key[V - 1];
-      order = taken ? order >> 2 : order;
-    } else {
+    for (int r = 0; r < kRuns; ++r) {
+      const bool here = taken & (kRuns == 1 || from == uint32_t(r));
 #pragma unroll
-      for (int i = 0; i < V; ++i)
-        if (taken && uint32_t(i) == j) key[i] = 0;
+      for (int i = r * kRun; i + 1 < (r + 1) * kRun; ++i)
+        key[i] = either(here, key[i + 1], key[i]);
+      key[(r + 1) * kRun - 1] = either(here, O(0), key[(r + 1) * kRun - 1]);
+      order[r] = either(here, order[r] >> 8, order[r]);
     }
   }
-  if (lane >= a.top_k) id = -1;
-  if (tol_abs == 0) return true;
-  // a round's value against the one before
-  const O before = __shfl_up(chosen, 1, 64);
-  close = close ||
-          (lane > 0 && chosen != 0 &&
-           too_close(K(from_order(before)), K(from_order(chosen)), 1, tol_abs,
-                     tol_rel));
-  return __ballot(close) == 0;
+  wave_order();
+  id = lane < a.top_k && chosen != 0 ? int(slot[lane]) : -1;
+  if (!inexact) return true;
+  // a round's value against the one before; that of round L is in no lane
+  const O before = __shfl_up(chosen, 1, L);
+  if (lane > 0 && chosen != 0)
+    close |= too_close(K(from_order(before)), K(from_order(chosen)), 1, tol_abs,
+                       tol_rel);
+  if (a.top_k == L && lane == L - 1 && last != 0)
+    close |= too_close(K(from_order(chosen)), K(from_order(last)), 1, tol_abs,
+                       tol_rel);
+  return team_bits<L>(close) == 0;
 }
 
 // The values that the choice compares, computed in K; returns tol.
-template <typename K, int V>
+template <typename K, int V, int L>
 __device__ __forceinline__ float values_of(const RouteArgs &a,
                                            const float (&l)[V], float top,
-                                           uint32_t lane, Order<K> (&key)[V]) {
+                                           uint32_t lane, bool vec_bias,
+                                           Order<K> (&key)[V]) {
   float tol = kTolSigmoid;
   K v[V];
   if (a.flags & CIERA_ROUTE_SIGMOID) {
@@ -268,98 +322,119 @@ __device__ __forceinline__ float values_of(const RouteArgs &a,
       v[j] = exp_of(K(l[j]) - K(top));
       sum += v[j];
     }
-    sum = one_over(wave_sum(sum));  // the largest score
+    sum = one_over(team_sum<L>(sum));  // the largest score
     tol = kTolSoftmax * float(sum);
 #pragma unroll
     for (int j = 0; j < V; ++j) v[j] *= sum;
   }
+  float b[V];
+  if (a.bias) {
+    load_logits<Fp32, V>(a.bias, a.n_experts, vec_bias, lane, b);
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j) b[j] = 0;
+  }
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const uint32_t e = lane * V + j;
-    const float b = a.bias && e < a.n_experts ? a.bias[e] : 0.0f;
-    const bool live = l[j] > -kInf && fabsf(b) < kInf;
-    key[j] = live ? to_order(v[j] + K(b)) : Order<K>(0);
+    const bool live = (l[j] > -kInf) & (fabsf(b[j]) < kInf);
+    key[j] = live ? to_order(v[j] + K(b[j])) : Order<K>(0);
   }
   return tol;
 }
 
-template <typename T, int V>
+template <typename T, int V, int L>
 __global__ void __launch_bounds__(64 * kWaves)
-    route_kernel(RouteArgs a, bool vec) {
-  __shared__ uint64_t shared[kWaves][64 * V];
-  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint32_t token = blockIdx.x * kWaves + wave;
-  if (token >= a.n_tokens) return;
+    route_kernel(RouteArgs a, bool vec, bool vec_bias) {
+  constexpr int kTeams = 64 / L;
+  constexpr int kWide = V / kTeams;  // experts a lane of a whole wave
+  __shared__ uint64_t shared[kWaves][64 * kWide];
+  __shared__ uint32_t slots[kWaves][64];
+  const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & (L - 1);
+  const uint32_t team = (threadIdx.x & 63) / L;
+  const uint32_t mine_token = (blockIdx.x * kWaves + wave) * kTeams + team;
+  if (mine_token - team >= a.n_tokens) return;
+  // a team without a token does the last one again
+  const bool real = mine_token < a.n_tokens;
+  const uint32_t token = real ? mine_token : a.n_tokens - 1;
+  const typename T::Raw *const row =
+      static_cast<const typename T::Raw *>(a.logits) +
+      uint64_t(token) * a.row_stride;
+  uint32_t *const slot = slots[wave] + team * L;
   float l[V];
-  load_logits<T, V>(static_cast<const typename T::Raw *>(a.logits) +
-                        token * a.row_stride,
-                    a.n_experts, vec, lane, l);
+  load_logits<T, V>(row, a.n_experts, vec, lane, l);
   float top = l[0];
   bool fine = l[0] < kInf;  // neither NaN nor +inf
 #pragma unroll
   for (int j = 1; j < V; ++j) {
     top = fmaxf(top, l[j]);
-    fine = fine && l[j] < kInf;
+    fine &= l[j] < kInf;
   }
-  const uint64_t out = uint64_t(token) * a.top_k + lane;
-  if (__ballot(!fine)) {
-    if (lane < a.top_k) {
-      a.ids[out] = -1;
-      a.weights[out] = __builtin_nanf("");
-    }
-    return;
-  }
-  top = wave_max(top);
+  fine = team_bits<L>(!fine) == 0;
+  top = from_order(team_max<L>(to_order(top)));
   const bool all_groups = a.top_groups == a.n_groups;
   const bool by_logit =
       !a.bias && (all_groups || !(a.flags & CIERA_ROUTE_GROUP_TOP_TWO));
   int id = -1;
-  if (top > -kInf) {
-    uint32_t key[V];
-    uint32_t *const room = reinterpret_cast<uint32_t *>(shared[wave]);
-    bool sure;
-    if (by_logit) {
+  uint32_t key[V];
+  uint32_t *const room = reinterpret_cast<uint32_t *>(shared[wave]);
+  float tol = 0;
+  if (by_logit) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) key[j] = l[j] > -kInf ? to_order(l[j]) : 0u;
-      sure = choose<float, V>(a, key, lane, room, 0.0f, 0.0f, id);
-    } else {
-      const float tol = values_of<float, V>(a, l, top, lane, key);
-      sure = choose<float, V>(a, key, lane, room, tol, kTolRel, id);
-    }
-    if (!sure) {
-      uint64_t wide[V];
-      values_of<double, V>(a, l, top, lane, wide);
-      choose<double, V>(a, wide, lane, shared[wave], 0.0f, 0.0f, id);
+    for (int j = 0; j < V; ++j) key[j] = l[j] > -kInf ? to_order(l[j]) : 0u;
+  } else {
+    tol = values_of<float, V, L>(a, l, top, lane, vec_bias, key);
+  }
+  const bool sure = choose<float, V, L>(a, key, lane, room, slot, !by_logit,
+                                        tol, kTolRel, id);
+  if (!by_logit) {
+    // again in fp64, a token after the other, the whole wave on each
+    for (uint64_t again = __ballot(!sure && fine && real && lane == 0);
+         again != 0; again &= again - 1) {
+      const int at = __builtin_ctzll(again);
+      const uint64_t its = __builtin_amdgcn_readlane(token, at);
+      const uint32_t all = threadIdx.x & 63;
+      float wide_l[kWide];
+      uint64_t wide[kWide];
+      load_logits<T, kWide>(static_cast<const typename T::Raw *>(a.logits) +
+                                its * a.row_stride,
+                            a.n_experts, vec, all, wide_l);
+      values_of<double, kWide, 64>(a, wide_l, lane_of(top, at), all, vec_bias,
+                                   wide);
+      int its_id;
+      wave_order();
+      choose<double, kWide, 64>(a, wide, all, shared[wave], slots[wave], false,
+                                0.0f, 0.0f, its_id);
+      its_id = __shfl(its_id, int(lane), 64);
+      if (int(team) == at / L) id = its_id;
     }
   }
   // the weights, from the chosen logits
-  const typename T::Raw *row =
-      static_cast<const typename T::Raw *>(a.logits) + token * a.row_stride;
   const bool chosen = id >= 0;
   const float mine = chosen ? T::to_float(row[id]) : -kInf;
   float w;
   if (a.flags & CIERA_ROUTE_NORMALIZE) {
     // softmax's own sum cancels. Below -30, where 1 + e^l rounds to 1, sigmoids
     // go as exponentials too; relative to the largest they cannot vanish.
-    const float high = wave_max(mine);
+    const float high = from_order(team_max<L>(to_order(mine)));
     float p = 0;
     if ((a.flags & CIERA_ROUTE_SIGMOID) && high > -30.0f)
       p = chosen ? 1.0f / (1.0f + expf(-mine)) : 0.0f;
     else
       p = chosen ? expf(mine - high) : 0.0f;
-    w = p / wave_sum(p);
+    w = p / team_sum<L>(p);
   } else if (a.flags & CIERA_ROUTE_SIGMOID) {
     w = 1.0f / (1.0f + expf(-mine));
   } else {
     float sum = 0;
 #pragma unroll
     for (int j = 0; j < V; ++j) sum += l[j] > -kInf ? expf(l[j] - top) : 0.0f;
-    sum = wave_sum(sum);
+    sum = team_sum<L>(sum);
     w = expf(mine - top) / sum;
   }
-  if (lane < a.top_k) {
-    a.ids[out] = id;
-    a.weights[out] = chosen ? w * a.scale : 0.0f;
+  if (real && lane < a.top_k) {
+    const uint64_t out = uint64_t(token) * a.top_k + lane;
+    a.ids[out] = fine ? id : -1;
+    a.weights[out] = !fine ? __builtin_nanf("") : chosen ? w * a.scale : 0.0f;
   }
 }
 
@@ -613,19 +688,30 @@ bool whole_reads(const void *p, uint64_t stride, uint32_t n, uint32_t V,
          reinterpret_cast<uintptr_t>(p) % align == 0;
 }
 
-template <typename T, int V>
+template <typename T, int V, int L>
 hipError_t route_wide(const RouteArgs &a, hipStream_t s) {
-  route_kernel<T, V><<<dim3((a.n_tokens + kWaves - 1) / kWaves),
-                       dim3(64 * kWaves), 0, s>>>(
-      a, whole_reads(a.logits, a.row_stride, a.n_experts, V, T::kBytes));
+  constexpr uint32_t kTokens = kWaves * (64 / L);  // per workgroup
+  route_kernel<T, V, L><<<dim3((a.n_tokens + kTokens - 1) / kTokens),
+                          dim3(64 * kWaves), 0, s>>>(
+      a, whole_reads(a.logits, a.row_stride, a.n_experts, V, T::kBytes),
+      whole_reads(a.bias, 0, a.n_experts, V, 4));
   return hipGetLastError();
+}
+// Whether V experts a lane in teams of 16 hold the tokens.
+bool in_rows(const RouteArgs &a, uint32_t V) {
+  return a.n_experts <= 16 * V && a.top_k <= 16 && a.n_tokens >= kRowTokens &&
+         (a.top_groups == a.n_groups ||
+          groups_in_row(a.n_experts / a.n_groups, V));
 }
 template <typename T>
 hipError_t route_typed(const RouteArgs &a, hipStream_t s) {
-  return a.n_experts <= 64    ? route_wide<T, 1>(a, s)
-         : a.n_experts <= 128 ? route_wide<T, 2>(a, s)
-         : a.n_experts <= 256 ? route_wide<T, 4>(a, s)
-                              : route_wide<T, 16>(a, s);
+  return in_rows(a, 4)        ? route_wide<T, 4, 16>(a, s)
+         : in_rows(a, 8)      ? route_wide<T, 8, 16>(a, s)
+         : in_rows(a, 16)     ? route_wide<T, 16, 16>(a, s)
+         : a.n_experts <= 64  ? route_wide<T, 1, 64>(a, s)
+         : a.n_experts <= 128 ? route_wide<T, 2, 64>(a, s)
+         : a.n_experts <= 256 ? route_wide<T, 4, 64>(a, s)
+                              : route_wide<T, 16, 64>(a, s);
 }
 
 template <typename T, int V>

@@ -148,6 +148,58 @@ def test_masked_logits(cl, o, E, bias):
     check(cl, l, 6, groups=4, top_groups=2, two=True, **o)
 
 
+def check_many(cl, rows, k, **o):
+    """As check(), with the rows again and again until there are so many tokens
+    that several share a wave, and every copy the same."""
+    R = rows.shape[0]
+    n = -(-4200 // R)
+    check(cl, rows, k, **o)
+    many = rows.repeat(n, 1)[:n * R - 3]
+    ids, w = route(cl, many.to(DEV), k, **dict(o))
+    ids_r, w_r = ref.route(rows, k, **dict(o))
+    assert torch.equal(ids, ids_r.repeat(n, 1)[:n * R - 3])
+    w_r = w_r.repeat(n, 1)[:n * R - 3]
+    assert torch.equal(torch.isnan(w), torch.isnan(w_r))
+    fine = ~torch.isnan(w_r)
+    # the bound of check(), with arguments of at most 110
+    bound = 2 * (116 + rows.shape[1]) * 2.0 ** -24
+    err = (w - w_r).abs()[fine]
+    assert (err <= bound * w_r.abs()[fine] + 2.0 ** -125).all()
+    first = torch.nan_to_num(w[:R])
+    for i in range(1, n - 1):  # a copy's bits do not depend on its place
+        assert torch.equal(torch.nan_to_num(w[i * R:(i + 1) * R]), first)
+
+
+@pytest.mark.parametrize("o", OPTIONS)
+@pytest.mark.parametrize("dtype,E,k,G,t,two", [
+    (torch.bfloat16, 8, 2, 1, 1, False), (torch.float32, 1, 1, 1, 1, False),
+    (torch.float16, 61, 6, 1, 1, False), (torch.bfloat16, 64, 16, 4, 3, True),
+    (torch.float32, 64, 8, 16, 5, True), (torch.bfloat16, 100, 17, 1, 1, False),
+    (torch.float32, 128, 16, 2, 1, True), (torch.float16, 130, 3, 1, 1, True),
+    (torch.float32, 256, 8, 8, 4, True), (torch.float32, 256, 16, 16, 9, False),
+    (torch.bfloat16, 252, 4, 12, 5, True), (torch.bfloat16, 257, 8, 1, 1, False)])
+def test_many_tokens(cl, o, dtype, E, k, G, t, two):
+    rows = randn(29, E, seed=E + k, std=2.0)
+    if E > 8:
+        rows[2, ::3] = -math.inf
+        rows[3] = -math.inf
+        rows[4, E - 2] = math.nan
+        rows[5, 1] = math.inf
+        rows[6:9] = rows[6:9].round()  # equals
+        rows[9] = 0.25
+        rows[10] = randn(E, seed=3) * 2.0 ** -20
+        rows[11] = -torch.finfo(dtype).max
+        rows[12, 2:] = -math.inf
+    rows = rows.to(dtype)
+    bias = randn(E, seed=5, std=0.05)
+    if E > 8:
+        bias[7] = math.nan
+    check_many(cl, rows, k, groups=G, top_groups=t, two=two, **o)
+    check_many(cl, rows, k, bias=bias, groups=G, top_groups=t, two=two, **o)
+    check_many(cl, rows, k, bias=torch.zeros(E), groups=G, top_groups=t,
+               two=two, **o)
+
+
 def test_strided_logits_and_a_side_stream(cl):
     wide = randn(50, 100, seed=1).to(torch.bfloat16).to(DEV)
     l = wide[:, 3:67]
