@@ -217,9 +217,6 @@ __device__ __forceinline__ double from_order(uint64_t o) {
   return __longlong_as_double((long long)(
       o ^ (o >> 63 ? 0x8000000000000000ull : 0xFFFFFFFFFFFFFFFFull)));
 }
-__device__ __forceinline__ float wave_max(float x) {
-  return from_order(wave_max(to_order(x)));
-}
 template <typename K>
 __device__ __forceinline__ K row_sum(K x) {  // in every lane of the row
   x += dpp<kDppPair>(K(0), x);

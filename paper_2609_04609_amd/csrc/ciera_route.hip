@@ -446,12 +446,12 @@ __global__ void __launch_bounds__(64 * kWaves)
 //   sigmoid              d_i = c s_i (1 - s_i) g_i
 // (d_i for the chosen; 0 elsewhere). Only the plain softmax reads the whole
 // row.
-template <typename T, int V>
+template <typename T, int V, int L>
 __global__ void __launch_bounds__(64 * kWaves)
-    route_backward_kernel(RouteBackArgs a, bool vec) {
-  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint32_t token = blockIdx.x * kWaves + wave;
-  if (token >= a.n_tokens) return;
+    route_backward_kernel(RouteBackArgs a, bool vec, bool vec_out) {
+  const uint32_t lane = threadIdx.x & (L - 1);
+  const uint32_t token = blockIdx.x * (64 / L * kWaves) + threadIdx.x / L;
+  if (token >= a.n_tokens) return;  // a whole team
   const typename T::Raw *row = static_cast<const typename T::Raw *>(a.logits) +
                                uint64_t(token) * a.row_stride;
   typename T::Raw *d_row = static_cast<typename T::Raw *>(a.d_logits) +
@@ -476,26 +476,26 @@ __global__ void __launch_bounds__(64 * kWaves)
 #pragma unroll
     for (int j = 0; j < V; ++j) top = l[j] > top || l[j] != l[j] ? l[j] : top;
     // a NaN stays the maximum's choice of no lane: the sum carries it instead
-    top = wave_max(top == top ? top : -kInf);
+    top = from_order(team_max<L>(to_order(top == top ? top : -kInf)));
     sum = 0;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       l[j] = l[j] == -kInf ? 0.0f : expf(l[j] - top);
       sum += l[j];
     }
-    sum = wave_sum(sum);
+    sum = team_sum<L>(sum);
     const float p = chosen && sum != 0 ? expf(mine - top) / sum : 0.0f;
     d = p * g;
-    spread = wave_sum(d);
+    spread = team_sum<L>(d);
   } else if (normal) {
-    const float high = wave_max(mine);
+    const float high = from_order(team_max<L>(to_order(mine)));
     const bool as_exp = !sigmoid || high <= -30.0f;
     const float s = sigmoid ? 1.0f / (1.0f + expf(-mine)) : 0.0f;
     float p = 0;
     if (chosen && high != -kInf) p = as_exp ? expf(mine - high) : s;
-    const float all = wave_sum(p);
+    const float all = team_sum<L>(p);
     const float w = all == 0 ? 0.0f : p / all;
-    const float mean = wave_sum(chosen ? w * g : 0.0f);
+    const float mean = team_sum<L>(chosen ? w * g : 0.0f);
     d = chosen ? w * (1.0f - s) * (g - mean) : 0.0f;
   } else {
     const float s = 1.0f / (1.0f + expf(-mine));
@@ -509,16 +509,25 @@ __global__ void __launch_bounds__(64 * kWaves)
     for (int j = 0; j < V; ++j) o[j] = sum != sum ? sum : 0.0f;
   }
   for (uint32_t s = 0; s < a.top_k; ++s) {
-    const int e = __builtin_amdgcn_readlane(id, int(s));
-    const float v = lane_of(d, int(s));
+    const int e = int(team_lane<L>(uint32_t(id), s));
+    const float v = team_lane<L>(d, s);
 #pragma unroll
     for (int j = 0; j < V; ++j)
       if (e == int(lane * V + j)) o[j] += v;
   }
+  typename T::Raw raw[V];
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    const uint32_t e = lane * V + j;
-    if (e < a.n_experts) d_row[e] = T::from_float(o[j]);
+  for (int j = 0; j < V; ++j) raw[j] = T::from_float(o[j]);
+  if (vec_out) {
+    if (lane * V < a.n_experts)
+      __builtin_memcpy(
+          __builtin_assume_aligned(d_row + lane * V,
+                                   V * T::kBytes < 16 ? V * T::kBytes : 16),
+          raw, V * T::kBytes);
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (lane * V + j < a.n_experts) d_row[lane * V + j] = raw[j];
   }
 }
 
@@ -714,19 +723,25 @@ hipError_t route_typed(const RouteArgs &a, hipStream_t s) {
                               : route_wide<T, 16, 64>(a, s);
 }
 
-template <typename T, int V>
+template <typename T, int V, int L>
 hipError_t route_back_wide(const RouteBackArgs &a, hipStream_t s) {
-  route_backward_kernel<T, V><<<dim3((a.n_tokens + kWaves - 1) / kWaves),
-                                dim3(64 * kWaves), 0, s>>>(
-      a, whole_reads(a.logits, a.row_stride, a.n_experts, V, T::kBytes));
+  constexpr uint32_t kTokens = kWaves * (64 / L);
+  route_backward_kernel<T, V, L>
+      <<<dim3((a.n_tokens + kTokens - 1) / kTokens), dim3(64 * kWaves), 0, s>>>(
+          a, whole_reads(a.logits, a.row_stride, a.n_experts, V, T::kBytes),
+          whole_reads(a.d_logits, a.d_row_stride, a.n_experts, V, T::kBytes));
   return hipGetLastError();
 }
 template <typename T>
 hipError_t route_back_typed(const RouteBackArgs &a, hipStream_t s) {
-  return a.n_experts <= 64    ? route_back_wide<T, 1>(a, s)
-         : a.n_experts <= 128 ? route_back_wide<T, 2>(a, s)
-         : a.n_experts <= 256 ? route_back_wide<T, 4>(a, s)
-                              : route_back_wide<T, 16>(a, s);
+  const bool rows = a.top_k <= 16 && a.n_tokens >= kRowTokens;
+  return rows && a.n_experts <= 64    ? route_back_wide<T, 4, 16>(a, s)
+         : rows && a.n_experts <= 128 ? route_back_wide<T, 8, 16>(a, s)
+         : rows && a.n_experts <= 256 ? route_back_wide<T, 16, 16>(a, s)
+         : a.n_experts <= 64          ? route_back_wide<T, 1, 64>(a, s)
+         : a.n_experts <= 128         ? route_back_wide<T, 2, 64>(a, s)
+         : a.n_experts <= 256         ? route_back_wide<T, 4, 64>(a, s)
+                                      : route_back_wide<T, 16, 64>(a, s);
 }
 
 }  // namespace

@@ -298,6 +298,41 @@ def test_gradient_of_odd_rows(cl, o):
         assert ((got[t] - x.grad[0]).abs() <= bound).all(), t
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("E,k,pad", [(8, 2, 0), (61, 16, 0), (64, 8, 0),
+                                     (64, 8, 3), (128, 17, 0), (100, 5, 4),
+                                     (256, 8, 0), (250, 12, 1)])
+@pytest.mark.parametrize("o", OPTIONS)
+def test_gradient_of_many_tokens(cl, dtype, E, k, pad, o):
+    """Enough tokens that several share a wave, rows `pad` values apart:
+    against the formula, with the bound of the few."""
+    R, T = 23, 4201
+    l = randn(R, E, seed=E, std=1.5).to(dtype)
+    l[1, E // 2:] = -math.inf
+    dw = randn(R, k, seed=2)
+    ids = torch.stack([torch.randperm(E, generator=torch.Generator(
+    ).manual_seed(t))[:k] for t in range(R)])
+    ids[1] = torch.arange(k) % (E // 2)  # of those not masked, some twice
+    at = torch.arange(T) % R
+    wide = torch.zeros(T, E + pad, dtype=dtype, device=DEV)
+    out = torch.full((T, E + pad), 3.0, dtype=dtype, device=DEV)
+    wide[:, :E] = l[at].to(DEV)
+    cl.route_backward_t(wide[:, :E], ids[at].int().to(DEV), dw[at].to(DEV),
+                        out[:, :E], **o)
+    got = out[:, :E].cpu().double()
+    assert (out[:, E:] == 3).all()
+    x = l.double().requires_grad_()
+    (ref.weights_of(x, ids, o.get("sigmoid", False), o.get("normalize", False),
+                    o.get("scale", 1.0)) * dw.double()).sum().backward()
+    exact = torch.nan_to_num(x.grad)
+    size = float(dw.abs().max()) * o.get("scale", 1.0)
+    bound = 4 * size * (12 + E + 9) * 2.0 ** -24 + \
+        torch.finfo(dtype).eps / 2 * exact.abs()
+    if dtype == torch.float16:
+        bound = bound + 2.0 ** -25
+    assert ((got - exact[at]).abs() <= bound[at]).all()
+
+
 # ----------------------------------------------------------------- plan ----
 
 @pytest.mark.parametrize("T,k,E,first", [
