@@ -286,16 +286,30 @@ __global__ void __launch_bounds__(256)
   }
   __syncthreads();
   Octet<T> o[8];
+  const uint8_t *const x = static_cast<const uint8_t *>(a.x);
+  if (tile_col + 128 <= a.n_cols && a.n_x > 0) {
+    // without a branch between them, so that all are in flight at once
+    uint32_t r[8];
 #pragma unroll
-  for (uint32_t i = 0; i < 8; ++i) {
-    const uint32_t r = row_of[t / 16 * 8 + i];
-    const uint8_t *x = static_cast<const uint8_t *>(a.x) +
-                       (uint64_t(r) * a.row_stride + c0) * T::kBytes;
-    if (r != kNone && c0 + 8 <= a.n_cols)
-      o[i].load(x);
-    else
-      o[i].load_some(x, r != kNone && c0 < a.n_cols ? uint32_t(a.n_cols - c0)
-                                                    : 0u);
+    for (uint32_t i = 0; i < 8; ++i) {
+      r[i] = row_of[t / 16 * 8 + i];
+      o[i].load(x + (uint64_t(r[i] == kNone ? 0 : r[i]) * a.row_stride + c0) *
+                        T::kBytes);
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i)
+      if (r[i] == kNone) o[i].clear();
+  } else {
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) {
+      const uint32_t r = row_of[t / 16 * 8 + i];
+      const uint8_t *at = x + (uint64_t(r) * a.row_stride + c0) * T::kBytes;
+      if (r != kNone && c0 + 8 <= a.n_cols)
+        o[i].load(at);
+      else
+        o[i].load_some(at, r != kNone && c0 < a.n_cols
+                               ? uint32_t(a.n_cols - c0) : 0u);
+    }
   }
   using M = Magnitude<T>;
   uint32_t m[M::kWords];
