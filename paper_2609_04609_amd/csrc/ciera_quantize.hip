@@ -43,6 +43,14 @@ struct Magnitude {
     else
       return w >= kInfinite << 16 || (w & 0xFFFFu) >= kInfinite;
   }
+  // a word whose infinities have become NaN
+  static __device__ __forceinline__ uint32_t without_infinity(uint32_t w) {
+    if constexpr (T::kBytes == 4)
+      return (w & 0x7FFFFFFFu) < kInfinite ? w : 0x7FFFFFFFu;
+    else
+      return ((w & 0x7FFFu) < kInfinite ? w & 0xFFFFu : 0x7FFFu) |
+             ((w >> 16 & 0x7FFFu) < kInfinite ? w & 0xFFFF0000u : 0x7FFF0000u);
+  }
   // the bits of the fp32 value of half h of a word (fp32: of the word)
   static __device__ __forceinline__ uint32_t wide(uint32_t w, uint32_t h) {
     if constexpr (T::kBytes == 4) return w;
@@ -241,28 +249,44 @@ __global__ void __launch_bounds__(256)
 }
 
 // -------------------------------------------------------------- columns ----
-// Four dwords of four bytes, transposed.
-__device__ __forceinline__ void transpose4(uint32_t &a, uint32_t &b, uint32_t &c,
-                                           uint32_t &d) {
-  const uint32_t ab_lo = __builtin_amdgcn_perm(b, a, 0x05010400u);  // a0 b0 a1 b1
-  const uint32_t ab_hi = __builtin_amdgcn_perm(b, a, 0x07030602u);  // a2 b2 a3 b3
-  const uint32_t cd_lo = __builtin_amdgcn_perm(d, c, 0x05010400u);
-  const uint32_t cd_hi = __builtin_amdgcn_perm(d, c, 0x07030602u);
-  a = __builtin_amdgcn_perm(cd_lo, ab_lo, 0x05040100u);
-  b = __builtin_amdgcn_perm(cd_lo, ab_lo, 0x07060302u);
-  c = __builtin_amdgcn_perm(cd_hi, ab_hi, 0x05040100u);
-  d = __builtin_amdgcn_perm(cd_hi, ab_hi, 0x07060302u);
+// Value k of two rows, divided by the scale and rounded, as two e4m3 bytes in the
+// upper (HIGH) or lower half of `old`: one instruction, whose operand is the two
+// values side by side.
+template <bool HIGH, typename T>
+__device__ __forceinline__ uint32_t pack_column(const Octet<T> &a,
+                                                const Octet<T> &b, uint32_t k,
+                                                float scale, uint32_t old) {
+  typedef short s16x2 __attribute__((ext_vector_type(2)));
+  const s16x2 o = __builtin_bit_cast(s16x2, old);
+  s16x2 r;
+  if constexpr (T::kBytes == 4) {
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(o, a.get(k), b.get(k), scale,
+                                                 HIGH);
+  } else {
+    const uint32_t two = __builtin_amdgcn_perm(
+        b.w[0][k / 2], a.w[0][k / 2], k % 2 ? 0x07060302u : 0x05040100u);
+    if constexpr (std::is_same_v<T, Bf16>) {
+      typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+      r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(
+          o, __builtin_bit_cast(bf16x2, two), scale, HIGH);
+    } else {
+      typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+      r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(
+          o, __builtin_bit_cast(f16x2, two), scale, HIGH);
+    }
+  }
+  return __builtin_bit_cast(uint32_t, r);
 }
 
 // A workgroup takes 128 rows of one expert and 128 columns, a thread 8 x 8 of
-// them, which it transposes in registers; LDS puts the columns' pieces of eight
-// bytes together. Block t of the columns belongs to the expert that the running sum
+// them, which the conversion takes by pairs of rows; LDS puts the columns' pieces of
+// eight bytes together. Block t of the columns belongs to the expert that the running sum
 // of rounded-up row counts puts it in, which every wave finds for itself.
 template <typename T>
 __global__ void __launch_bounds__(256)
     quantize_columns_kernel(QuantColumnsArgs a, uint32_t col_tiles) {
   __shared__ uint32_t top[4][128];
-  __shared__ float inverse[128];
+  __shared__ float scale_of[128];
   __shared__ uint32_t row_of[128];
   // column c's piece of rows 8 g on at place g ^ (c / 8 % 16)
   __shared__ u32x2 tile[128][16];
@@ -349,39 +373,28 @@ __global__ void __launch_bounds__(256)
 #pragma unroll
     for (int w = 1; w < 4; ++w) word = M::larger(word, top[w][t / kHalves]);
     const uint32_t byte = scale_byte(M::wide(word, t % kHalves));
-    inverse[t] = inverse_scale(byte);
+    scale_of[t] = __uint_as_float(byte << 23);  // the exponent alone is read
     if (tile_col + t < a.n_cols)
       a.scales[uint64_t(tile_col + t) * a.scale_stride + block] = uint8_t(byte);
   }
   __syncthreads();
-  float inv[8];
-#pragma unroll
-  for (int k = 0; k < 8; ++k) inv[k] = inverse[(t % 16) * 8 + k];
-  uint32_t q[8][2];
   if (any) {
 #pragma unroll
-    for (uint32_t i = 0; i < 8; ++i) {
-      const u32x2 v = octet_e4m3<true>(o[i], inv);
-      q[i][0] = v[0];
-      q[i][1] = v[1];
-    }
-  } else {
+    for (uint32_t i = 0; i < 8; ++i)
 #pragma unroll
-    for (uint32_t i = 0; i < 8; ++i) {
-      const u32x2 v = octet_e4m3<false>(o[i], inv);
-      q[i][0] = v[0];
-      q[i][1] = v[1];
-    }
+      for (uint32_t w = 0; w < M::kWords; ++w)
+        o[i].w[w / 4][w % 4] = M::without_infinity(o[i].w[w / 4][w % 4]);
   }
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    transpose4(q[0][h], q[1][h], q[2][h], q[3][h]);
-    transpose4(q[4][h], q[5][h], q[6][h], q[7][h]);
+  for (uint32_t k = 0; k < 8; ++k) {
+    const float scale = scale_of[(t % 16) * 8 + k];
+    u32x2 q;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const uint32_t c = (t % 16) * 8 + 4 * h + k;
-      tile[c][(t / 16) ^ (t % 16)] = u32x2{q[k][h], q[4 + k][h]};
+    for (uint32_t h = 0; h < 2; ++h) {
+      const uint32_t two = pack_column<false>(o[4 * h], o[4 * h + 1], k, scale, 0);
+      q[h] = pack_column<true>(o[4 * h + 2], o[4 * h + 3], k, scale, two);
     }
+    tile[(t % 16) * 8 + k][(t / 16) ^ (t % 16)] = q;
   }
   __syncthreads();
 #pragma unroll

@@ -206,6 +206,40 @@ def test_columns(cl, dtype, counts, C, gather):
     assert (st[:, at // 128:] == 0xA5).all()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_every_value_rounds_right_in_columns(cl, dtype):
+    """All finite 16-bit values (of fp32: bits at random, the upper half counted
+    through), each in a column whose scale it sets, next to an infinity, and in one
+    whose maximum is some powers of two larger."""
+    bits = torch.arange(65536, dtype=torch.int64)
+    if dtype == torch.float32:
+        g = torch.Generator().manual_seed(1)
+        bits = bits * 65536 + torch.randint(0, 65536, (65536,), generator=g)
+        bits = torch.where(bits >= 2 ** 31, bits - 2 ** 32, bits)
+        v = bits.to(torch.int32).view(dtype)
+    else:
+        v = bits.to(torch.int16).view(dtype)
+    v = v[torch.isfinite(v)]
+    n = v.numel()
+    x = torch.zeros(3 * 130, n, dtype=dtype)
+    x[5] = v
+    x[130 + 127] = v
+    x[130 + 8, ::2] = math.inf
+    x[130 + 9, 1::3] = -math.inf
+    x[260 + 64] = v
+    a = v.abs().double()
+    f = torch.finfo(dtype)
+    x[260 + 77] = torch.where((a > 0) & (a < f.max / 2.0 ** 9), a * 2.0 ** 7,
+                              a).to(dtype)
+    off = torch.tensor([0, 130, 260, 390], dtype=torch.int32)
+    qt, st = narrow(n, cl.ciera_columns_length(390, 3))
+    cl.quantize_columns_t(x.to(DEV), off.to(DEV), qt, st)
+    for e in range(3):
+        qr, sr = ref.quantize(x[130 * e:130 * (e + 1)], 128, 1)
+        same(qt[:, 256 * e:256 * e + 130].float(), qr.t())
+        assert torch.equal(st[:, 2 * e:2 * e + 2].cpu().long(), sr.t())
+
+
 # -------------------------------------------------------------- products ----
 
 def whole_values(rows, cols, filled, seed, per_row=1):
