@@ -109,22 +109,6 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t amax) {
   const int e = int(amax >> 23) - 8 + ((amax & 0x7FFFFFu) > 0x600000u ? 1 : 0);
   return e > 0 ? uint32_t(e) : 0u;
 }
-// 2^-e of a scale byte: 2^(127 - byte), normal for bytes up to 253; the largest
-// byte is 127 + 120
-__device__ __forceinline__ float inverse_scale(uint32_t byte) {
-  return __uint_as_float((254u - byte) << 23);
-}
-// Four e4m3 bytes. Values are within +-448 (so nothing saturates) or not
-// finite, which become NaN.
-__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c,
-                                              float d) {
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-  return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true));
-}
-__device__ __forceinline__ float times(float x, float inv) {
-  // an infinity may not become a saturated value
-  return fabsf(x) < __builtin_inff() ? x * inv : __builtin_nanf("");
-}
 
 // ------------------------------------------------------ across a wave ----
 // DPP controls: the other lane of a pair or of a pair of pairs, the mirrored
