@@ -2,6 +2,8 @@
 
 The codec itself lives in ``libciera.so`` (hand-written HIP kernels behind a
 C ABI, declared in ``include/ciera.h``); ``ciera`` is its ctypes binding and
-``synth`` the seeded input generators. Importing the package loads nothing:
+``synth`` the seeded input generators. ``pipeline`` overlaps the codec with a
+link and compute; ``experts`` is a layer of experts over decoded weights, of the
+experts' operators in ``ciera``. Importing the package loads nothing:
 the library is opened on first use and a missing build raises.
 """
