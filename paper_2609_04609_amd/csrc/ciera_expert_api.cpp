@@ -38,6 +38,9 @@ bool narrow_ok(const void *q, uint64_t stride, const uint8_t *scales,
 // 32-bit quantities inside the kernels: rows, columns and grid sizes
 constexpr uint64_t kMost = uint64_t(1) << 31;
 constexpr uint64_t kMostCols = uint64_t(1) << 30;
+// a launch has fewer than 2^32 threads: workgroups of 256, and their waves
+constexpr uint64_t kMostGroups = uint64_t(1) << 24;
+constexpr uint64_t kMostWaves = 4 * kMostGroups;
 bool ints_ok(const void *p) { return p && aligned(p, 4); }
 int status(hipError_t e) { return e == hipSuccess ? CIERA_OK : CIERA_EHIP; }
 
@@ -59,7 +62,8 @@ int ciera_route(const void *logits, uint32_t dtype, uint64_t n_tokens,
       top_groups == 0 || top_groups > n_groups || top_k == 0 ||
       top_k > CIERA_MAX_TOP_K || top_k > n_experts / n_groups * top_groups)
     return CIERA_EINVAL;
-  if (dtype > CIERA_DT_FP32 || n_tokens >= kMost || n_tokens * top_k >= kMost)
+  if (dtype > CIERA_DT_FP32 || n_tokens >= kMostWaves ||
+      n_tokens * top_k >= kMost)
     return CIERA_EINVAL;
   if (n_tokens == 0) return CIERA_OK;
   if (!wide_ok(logits, dtype, n_experts, row_stride) || !aligned(bias, 4) ||
@@ -82,8 +86,8 @@ int ciera_route_backward(const void *logits, uint32_t dtype,
   if (flags & ~(CIERA_ROUTE_SIGMOID | CIERA_ROUTE_NORMALIZE))
     return CIERA_EINVAL;
   if (n_experts == 0 || n_experts > CIERA_MAX_EXPERTS || top_k == 0 ||
-      top_k > CIERA_MAX_TOP_K || dtype > CIERA_DT_FP32 || n_tokens >= kMost ||
-      n_tokens * top_k >= kMost)
+      top_k > CIERA_MAX_TOP_K || dtype > CIERA_DT_FP32 ||
+      n_tokens >= kMostWaves || n_tokens * top_k >= kMost)
     return CIERA_EINVAL;
   if (n_tokens == 0) return CIERA_OK;
   if (!wide_ok(logits, dtype, n_experts, row_stride) ||
@@ -131,7 +135,7 @@ int ciera_quantize_rows(const void *x, uint32_t dtype, uint64_t n_rows,
                         uint8_t *scales, uint64_t scale_stride,
                         hipStream_t stream) {
   CallScope scope;
-  if (dtype > CIERA_DT_FP32 || n_rows >= kMost || n_cols >= kMostCols ||
+  if (dtype > CIERA_DT_FP32 || n_rows >= kMostWaves || n_cols >= kMostCols ||
       q_rows >= kMost || top_k == 0 || top_k > CIERA_MAX_TOP_K ||
       (!position && (top_k != 1 || q_rows < n_rows)))
     return CIERA_EINVAL;
@@ -158,7 +162,7 @@ int ciera_quantize_blocks(const void *w, uint32_t dtype, uint64_t batch,
     return CIERA_EINVAL;
   if (batch == 0 || n_rows == 0 || n_cols == 0) return CIERA_OK;
   const uint64_t rb = (n_rows + 127) / 128, cb = (n_cols + 127) / 128;
-  if (rb * cb >= kMost || batch * rb * cb >= kMost) return CIERA_EINVAL;
+  if (rb * cb >= kMostGroups || batch * rb * cb >= kMostGroups) return CIERA_EINVAL;
   if (!wide_ok(w, dtype, n_cols, n_cols) ||
       !narrow_ok(q, q_stride, scales, scale_stride, up128(n_cols)) ||
       (q_t &&
@@ -192,7 +196,7 @@ int ciera_quantize_columns(const void *x, uint32_t dtype, uint64_t n_x,
   const uint64_t need = ciera_columns_length(n_rows, n_experts);
   if (length < need) return CIERA_ENOSPC;
   if (n_rows == 0 || n_cols == 0) return CIERA_OK;
-  if (need / 128 * ((n_cols + 127) / 128) >= kMost) return CIERA_EINVAL;
+  if (need / 128 * ((n_cols + 127) / 128) >= kMostGroups) return CIERA_EINVAL;
   if (!wide_ok(x, dtype, n_cols, row_stride) || !aligned(source, 4) ||
       !ints_ok(offsets) || !narrow_ok(q_t, length, scales, scale_stride, length))
     return CIERA_EINVAL;
@@ -219,8 +223,8 @@ int ciera_expert_matmul(const void *a, uint64_t a_stride,
       (!offsets && n_experts != 1))
     return CIERA_EINVAL;
   if (n_rows == 0 || n_out == 0) return CIERA_OK;
-  // a workgroup for every 16 rows and 16 columns is the most that is launched
-  if (((n_rows + 15) / 16 + n_experts) * ((n_out + 15) / 16) >= kMost)
+  // tiles of 128 x 128; the kernel of few rows looks for itself
+  if (((n_rows + 127) / 128 + n_experts) * ((n_out + 127) / 128) >= kMostGroups)
     return CIERA_EINVAL;
   if (!narrow_ok(a, a_stride, a_scales, a_scale_stride, depth) ||
       !narrow_ok(b, b_stride, b_scales, b_scale_stride, depth) ||
@@ -247,7 +251,7 @@ int ciera_expert_weight_grad(const void *dy_t, const uint8_t *dy_scales,
       length % 128 != 0 || length >= kMost)
     return CIERA_EINVAL;
   if (n_out == 0 || n_cols == 0) return CIERA_OK;
-  if ((n_out + 127) / 128 * ((n_cols + 127) / 128) >= kMost / n_experts)
+  if ((n_out + 127) / 128 * ((n_cols + 127) / 128) >= kMostGroups / n_experts)
     return CIERA_EINVAL;
   // without columns nothing is read from the operands, which may be null
   if (length > 0 &&
@@ -273,7 +277,7 @@ int ciera_combine(const void *rows, uint32_t dtype, uint64_t n_rows,
       n_tokens * top_k >= kMost)
     return CIERA_EINVAL;
   if (n_tokens == 0 || n_cols == 0) return CIERA_OK;
-  if (n_tokens * ((n_cols + 511) / 512) >= kMost) return CIERA_EINVAL;
+  if (n_tokens * ((n_cols + 511) / 512) >= kMostWaves) return CIERA_EINVAL;
   if ((n_rows > 0 && !wide_ok(rows, dtype, n_cols, row_stride)) ||
       !wide_ok(out, dtype, n_cols, out_stride) || !aligned(weights, 4) ||
       !ints_ok(position))
@@ -293,7 +297,7 @@ int ciera_combine_backward(const void *d_out, uint64_t d_out_stride,
   CallScope scope;
   if (dtype > CIERA_DT_FP32 || n_rows >= kMost || n_cols >= kMostCols ||
       top_k == 0 || top_k > CIERA_MAX_TOP_K || n_tokens >= kMost ||
-      n_tokens * top_k >= kMost)
+      n_tokens * top_k >= kMostWaves)
     return CIERA_EINVAL;
   if (n_tokens == 0) return CIERA_OK;
   if (!ints_ok(weights) || !ints_ok(position) || !ints_ok(d_weights))

@@ -1098,6 +1098,7 @@ bool many_tiles(uint64_t rows, uint64_t cols) {
 template <typename T, int FR, int SPLIT>
 hipError_t few_split(const MatmulArgs &a, uint32_t tiles, hipStream_t s) {
   const uint32_t groups = uint32_t((a.n_out + 64 / SPLIT - 1) / (64 / SPLIT));
+  if (uint64_t(tiles) * groups * 256 >> 32) return hipErrorInvalidConfiguration;
   few_rows_kernel<T, FR, SPLIT><<<dim3(tiles * groups), dim3(256), 0, s>>>(
       a, groups, aligned_fours(a.out, a.out_stride, T::kBytes));
   return hipGetLastError();

@@ -186,3 +186,19 @@ def test_the_reference_itself():
     o, s, p = ref.plan(torch.tensor([[1, 0], [5, 1]]), 2)
     assert o.tolist() == [0, 1, 3] and s.tolist() == [1, 0, 3, -1]
     assert p.tolist() == [[1, 0], [-1, 2]]
+
+
+def test_launches_past_32_bits_of_threads(cl):
+    """Sizes that a device's memory could hold but one launch could not cover."""
+    big = 1 << 26
+    assert cl.ciera_route(P, 0, big, 1, 1, 0, 1, 1, 1, 0, 1.0, P, P,
+                          0) == cl.EINVAL
+    assert cl.ciera_route_backward(P, 0, big, 1, 1, 1, 0, 1.0, P, P, P, 1,
+                                   0) == cl.EINVAL
+    assert cl.ciera_quantize_rows(P, 0, big, 128, 128, 0, 1, big, P, 128, P, 4,
+                                  0) == cl.EINVAL
+    assert cl.ciera_quantize_blocks(P, 0, 1 << 24, 1, 128, P, 128, P, 4, 0, 0,
+                                    0, 0, 0) == cl.EINVAL
+    assert cl.ciera_combine(P, 0, 1, 8, 8, P, P, big, 1, P, 8, 0) == cl.EINVAL
+    assert cl.ciera_combine_backward(P, 8, P, 0, 1, 8, 8, P, P, big // 8, 8, P,
+                                     8, P, 0) == cl.EINVAL
