@@ -472,27 +472,21 @@ __global__ void __launch_bounds__(256)
 // Rn and Cn are halves of the rows' and columns' fragments; each is read while the
 // quadrant before it is multiplied. One barrier a block, behind the last read of
 // its stage and the arrival of the next one. The results of a tile are stored
-// while the next tile's first block is multiplied, a quadrant ahead of the
-// instructions that overwrite it.
+// while the next tile's first block is multiplied: those of its upper half in front of
+// the first quadrant, which overwrites them, the others during the first two.
 struct Stream {
   static constexpr int TR = 256, TC = 256;
   static constexpr int kStage = (TR + TC) * 128;
   static constexpr int kScales = (TR + TC) * 4;
-  // loads of a wave behind the last that is waited for, and stores of a quadrant
-  static constexpr int kBehind = 18, kStores = 8;
+  // loads of a wave behind the last that is waited for, and stores of a tile
+  static constexpr int kBehind = 18, kStores = 32;
 };
 
-// Columns of a fragment. Row p = 4 u + i of fragment g is column 32 (g / 2) + 8 u
-// + 4 (g % 2) + i, so that a lane's results of two fragments are eight
-// neighbours: one 16-byte store. Chunk c of a column lies in LDS at c ^ col_key: the
-// 16 of a fragment then cover all banks.
-__device__ __forceinline__ constexpr uint32_t col_of(uint32_t p, uint32_t g) {
-  return 32 * (g >> 1) + 8 * (p >> 2) + 4 * (g & 1) + (p & 3);
-}
-__device__ __forceinline__ constexpr uint32_t col_key(uint32_t row) {
-  return ((row >> 1) & 1) | ((row >> 3) & 3) << 1;
-}
-
+// A tile's columns are loaded so that fragment g of a wave's 128 has column 8 p + g
+// for lane p: its eight results of a row are neighbours, one 16-byte store, and go on
+// in the next lane. (Lanes p in different rows: 64 clocks a store instead of 16, 880
+// us instead of 832 for 65,536 rows x 7168 x 2048.) In LDS a row of either operand has
+// the place that its fragment and lane give it.
 // Raw 32-bit buffer: reads past `bytes` give 0, writes there are dropped. Its
 // words are the same in all lanes, which the compiler is told here: else it loops
 // over the lanes' values.
@@ -726,13 +720,13 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
   // A wave loads 32 rows of each half of both operands, as 4 instructions of 8.
   const uint32_t row_stride = what.row_stride(), col_stride = what.col_stride();
   const uint32_t wave_row = (wave >> 1) * 128 + (wave & 1) * 32;
-  uint32_t row_at[2], col_at[4];
+  uint32_t row_at[2], col_at[2];
 #pragma unroll
-  for (uint32_t i = 0; i < 4; ++i) {
+  for (uint32_t i = 0; i < 2; ++i) {
     const uint32_t r = wave_row + i * 8 + (lane >> 3);
-    if (i < 2)
-      row_at[i] = r * row_stride + (((lane & 7) ^ ((r >> 1) & 7)) << 4);
-    col_at[i] = r * col_stride + (((lane & 7) ^ col_key(r)) << 4);
+    const uint32_t chunk = ((lane & 7) ^ ((r >> 1) & 7)) << 4;
+    row_at[i] = r * row_stride + chunk;
+    col_at[i] = ((r & 128) + 8 * (r & 15) + (r >> 4 & 7)) * col_stride + chunk;
   }
   // Scales: place 8 p + f of a half of 128 holds the dword of the row that lane p
   // has in fragment f, so that a lane's eight are two 16-byte reads.
@@ -741,8 +735,7 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
       ((wave >> 1) * 128 + 16 * (place & 7) + (place >> 3)) *
       what.row_scale_stride();
   const uint32_t col_scale_at =
-      (P::kColBlocks ? wave >> 1
-                     : (wave >> 1) * 128 + col_of(place >> 3, place & 7)) *
+      (P::kColBlocks ? wave >> 1 : (wave >> 1) * 128 + place) *
       what.col_scale_stride();
   u32x4 rr, rc, rrs, rcs;
   uint32_t bytes_r, bytes_c, bytes_rs, bytes_cs, real, load_phase;
@@ -785,10 +778,11 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
                                           kb * 128);
   };
   const auto load_col = [&](auto h, auto i, auto stage, uint32_t kb) {
-    constexpr uint32_t n = decltype(i)::value;
-    constexpr uint32_t half = 64 * decltype(h)::value;
-    buffer_to_lds16<decltype(stage)::value * Stream::kStage + (half + 8 * n) * 128>(
-        rc, lds_cols, col_at[n], half * col_stride, kb * 128);
+    constexpr uint32_t n = decltype(i)::value, half = 64 * decltype(h)::value;
+    buffer_to_lds16<decltype(stage)::value * Stream::kStage +
+                    (half + 8 * n) * 128>(rc, lds_cols, col_at[n & 1],
+                                          (half / 16 + n / 2) * col_stride,
+                                          kb * 128);
   };
   const auto load_scales = [&](auto stage, uint32_t kb) {
     constexpr uint32_t at = decltype(stage)::value * Stream::kScales;
@@ -807,11 +801,8 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
   const uint32_t p = lane & 15, quarter = lane >> 4;
   const uint32_t row_lo = place_of(row0 + p, quarter);
   const uint32_t row_hi = place_of(row0 + p, quarter + 4);
-  const uint32_t col_row = col0 + col_of(p, 0);
-  const uint32_t col_lo = Stream::TR * 128 + col_row * 128 +
-                          ((quarter ^ col_key(col_row)) << 4);
-  const uint32_t col_hi = Stream::TR * 128 + col_row * 128 +
-                          (((quarter + 4) ^ col_key(col_row)) << 4);
+  const uint32_t col_lo = Stream::TR * 128 + place_of(col0 + p, quarter);
+  const uint32_t col_hi = Stream::TR * 128 + place_of(col0 + p, quarter + 4);
   const auto joined = [&](uint32_t lo_at, uint32_t hi_at) -> i32x8 {
     const i32x4 lo = *reinterpret_cast<const i32x4 *>(lds + lo_at);
     const i32x4 hi = *reinterpret_cast<const i32x4 *>(lds + hi_at);
@@ -822,7 +813,7 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
     return joined(row_lo + at, row_hi + at);
   };
   const auto read_col = [&](uint32_t g, uint32_t stage) -> i32x8 {
-    const uint32_t at = stage * Stream::kStage + col_of(0, g) * 128;
+    const uint32_t at = stage * Stream::kStage + g * 2048;
     return joined(col_lo + at, col_hi + at);
   };
   // dwords of scales: rows' fragments 0 ... 7, then columns'
@@ -853,8 +844,8 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
       f32x4 &d = acc[4 * hr + f][4 * hc + g];
       const f32x4 zero = {0, 0, 0, 0};
       d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-          c[g], r[f], decltype(first)::value ? zero : d, 0, 0, 0,
-          int(sc[kNow][4 * hc + g]), 0, int(sr[kNow][4 * hr + f]));
+          r[f], c[g], decltype(first)::value ? zero : d, 0, 0, 0,
+          int(sr[kNow][4 * hr + f]), 0, int(sc[kNow][4 * hc + g]));
       // keeps its place among the loads, which are volatile as well
       asm volatile("" : "+a"(d));
     }
@@ -863,10 +854,9 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
   Job held{0, 0, 0, 0, 0, 0, 4};
   const uint32_t out_stride = uint32_t(what.out_stride()) * T::kBytes;
   const uint32_t out_at =
-      (row0 + p) * out_stride + (col0 + 8 * quarter) * T::kBytes;
-  // piece i < 8 of a quadrant: a rows' fragment, eight columns a lane
-  const auto store = [&](int hr, int hc, int i) {
-    const int f = i / 2, g = 2 * (i % 2);
+      (row0 + 4 * quarter) * out_stride + (col0 + 8 * p) * T::kBytes;
+  // row 16 f + i of every 16 of the wave, eight columns a lane
+  const auto store = [&](int f, int i) {
     uint32_t stride = out_stride;
     asm volatile("" : "+s"(stride));  // what follows from it is not kept
     const u32x4 words =
@@ -879,18 +869,13 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
         words[2], words[3]);
     u32x4 w;
 #pragma unroll
-    for (int h = 0; h < 4; ++h) {
-      const f32x4 v = acc[4 * hr + f][4 * hc + g + h / 2];
-      w[h] = pack_pair<T>(v[2 * (h % 2)], v[2 * (h % 2) + 1]);
-    }
+    for (int h = 0; h < 4; ++h)
+      w[h] = pack_pair<T>(acc[f][2 * h][i], acc[f][2 * h + 1][i]);
     // dropped by the range check where there is no such row or column
-    const bool there =
-        int(p) < int(held.rows - row0) - 64 * hr - 16 * f &&
-        int(8 * quarter) <
-            int(what.n_cols() - held.col - col0) - 64 * hc - 16 * g;
-    __builtin_amdgcn_raw_buffer_store_b128(
-        w, out, there ? out_at : ~0u,
-        (64 * hr + 16 * f) * stride + (64 * hc + 16 * g) * T::kBytes, 0);
+    const bool there = int(4 * quarter) < int(held.rows - row0) - 16 * f - i &&
+                       int(8 * p) < int(what.n_cols() - held.col - col0);
+    __builtin_amdgcn_raw_buffer_store_b128(w, out, there ? out_at : ~0u,
+                                           (16 * f + i) * stride, 0);
   };
 
   // A block of the tile, in stage 0 or 1. It loads block load_kb of the tile that is
@@ -912,18 +897,21 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
     constexpr uint32_t kNow = decltype(stage)::value, kNext = kNow ^ 1;
     i32x8(&c0)[4] = cs[kNow];
     i32x8(&c1)[4] = cs[kNext];
-    // a quarter of a quadrant of the last tile's results
-    const auto old = [&](int hr, int hc, int i) {
+    // two rows' stores of the last tile's results
+    const auto old = [&](uint32_t n) {
       if constexpr (kFirst) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          store(hr, hc, 2 * i + k);
+        for (uint32_t k = 2 * n; k < 2 * n + 2; ++k) {
+          store(k / 4, k % 4);
           in_order();
         }
       }
     };
     point(load_kb);
-    each([&](auto i) { old(0, 0, i.value); });
+    each([&](auto i) {
+      old(2 * i.value);
+      old(2 * i.value + 1);
+    });
     in_order();
     each([&](auto i) {
       c1[i.value] = read_col(4 + i.value, kNow);
@@ -933,14 +921,14 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
       load_col(even, i, stage, load_kb);
       multiply(first, stage, 0, 0, r0, c0, 4 * i.value + 2, 2);
       in_order();
-      old(0, 1, i.value);
+      old(8 + i.value);
     });
     load_scales(stage, load_kb);
     each([&](auto i) {
       r1[i.value] = read_row(4 + i.value, kNow);
       multiply(first, stage, 0, 1, r0, c1, 2 * i.value, 2);
       in_order();
-      old(1, 1, i.value);
+      old(12 + i.value);
     });
     multiply(first, stage, 0, 1, r0, c1, 8, 8);
     in_order();
@@ -948,7 +936,7 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
     // second half of this one. Behind those loads there are others, and a tile's
     // stores.
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier"
-                 :: "i"(Stream::kBehind + (kFirst ? 3 * Stream::kStores : 0)) : "memory");
+                 :: "i"(Stream::kBehind + (kFirst ? Stream::kStores : 0)) : "memory");
     in_order();
     u32x4 scales[4];
     read_scales(scales, kNext);
@@ -957,7 +945,6 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
       load_row(odd, i, stage, load_kb);
       multiply(first, stage, 1, 1, r1, c1, 4 * i.value, 4);
       in_order();
-      old(1, 0, i.value);
     });
     each([&](auto i) {
       c1[i.value] = read_col(i.value, kNext);
@@ -971,7 +958,7 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
     in_order();
     // the same of the second half of the next block, and the first half of it
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier"
-                 :: "i"(Stream::kBehind + (kFirst ? 4 * Stream::kStores : 0)) : "memory");
+                 :: "i"(Stream::kBehind + (kFirst ? Stream::kStores : 0)) : "memory");
     in_order();
   };
 
@@ -1021,12 +1008,7 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
     job = next;
   } while (job.rows != 0);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    store(0, 0, i);
-    store(0, 1, i);
-    store(1, 1, i);
-    store(1, 0, i);
-  }
+  for (int k = 0; k < 32; ++k) store(k / 4, k % 4);
 }
 
 // Where an expert's columns start and how many there are, in blocks of 128
