@@ -711,6 +711,13 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
   const uint32_t wave = same(threadIdx.x >> 6);
   if (wave == 0) what.prepare(sums, lane);
   __syncthreads();
+  // The lane, counted anew where little follows from it: every register is taken, and a
+  // value that is put aside comes back with a wait for all loads and stores.
+  const auto lane_again = [] {
+    uint32_t l = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0));
+    asm volatile("" : "+v"(l));
+    return l;
+  };
   // the XCD's share of the grid's tiles, and the workgroup's place in it
   uint32_t tile = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
   Job job = what.job(sums, tile, lane);
@@ -728,15 +735,6 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
     row_at[i] = r * row_stride + chunk;
     col_at[i] = ((r & 128) + 8 * (r & 15) + (r >> 4 & 7)) * col_stride + chunk;
   }
-  // Scales: place 8 p + f of a half of 128 holds the dword of the row that lane p
-  // has in fragment f, so that a lane's eight are two 16-byte reads.
-  const uint32_t place = (wave & 1) * 64 + lane;
-  const uint32_t row_scale_at =
-      ((wave >> 1) * 128 + 16 * (place & 7) + (place >> 3)) *
-      what.row_scale_stride();
-  const uint32_t col_scale_at =
-      (P::kColBlocks ? wave >> 1 : (wave >> 1) * 128 + place) *
-      what.col_scale_stride();
   u32x4 rr, rc, rrs, rcs;
   uint32_t bytes_r, bytes_c, bytes_rs, bytes_cs, real, load_phase;
   // the tile that is loaded from now on; without one nothing is read
@@ -787,8 +785,16 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
   const auto load_scales = [&](auto stage, uint32_t kb) {
     constexpr uint32_t at = decltype(stage)::value * Stream::kScales;
     const uint32_t dword = (load_phase + kb) & ~3u;
-    buffer_to_lds4<at>(rrs, lds_row_scales, row_scale_at, dword);
-    buffer_to_lds4<at>(rcs, lds_col_scales, col_scale_at, dword);
+    // Place 8 p + f of a half of 128 holds the dword of the row that lane p has in
+    // fragment f, so that a lane's eight are two 16-byte reads.
+    const uint32_t place = (wave & 1) * 64 + lane_again();
+    buffer_to_lds4<at>(rrs, lds_row_scales,
+                       ((wave >> 1) * 128 + 16 * (place & 7) + (place >> 3)) *
+                           what.row_scale_stride(),
+                       dword);
+    uint32_t col = P::kColBlocks ? wave >> 1 : (wave >> 1) * 128 + place;
+    if constexpr (P::kColBlocks) asm volatile("" : "+s"(col));
+    buffer_to_lds4<at>(rcs, lds_col_scales, col * what.col_scale_stride(), dword);
   };
 
   // ---- multiplying ----
@@ -819,8 +825,9 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
   // dwords of scales: rows' fragments 0 ... 7, then columns'
   const auto read_scales = [&](u32x4(&to)[4], uint32_t stage) {
     const uint8_t *s = lds + 2 * Stream::kStage + stage * Stream::kScales;
-    const uint8_t *r = s + (row0 + 8 * p) * 4;
-    const uint8_t *c = s + (Stream::TR + col0 + 8 * p) * 4;
+    const uint32_t at = (lane_again() & 15) * 32;
+    const uint8_t *r = s + row0 * 4 + at;
+    const uint8_t *c = s + (Stream::TR + col0) * 4 + at;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       to[h] = *reinterpret_cast<const u32x4 *>(r + 16 * h);
@@ -853,8 +860,6 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
   // the tile whose results are still in registers
   Job held{0, 0, 0, 0, 0, 0, 4};
   const uint32_t out_stride = uint32_t(what.out_stride()) * T::kBytes;
-  const uint32_t out_at =
-      (row0 + 4 * quarter) * out_stride + (col0 + 8 * p) * T::kBytes;
   // row 16 f + i of every 16 of the wave, eight columns a lane
   const auto store = [&](int f, int i) {
     uint32_t stride = out_stride;
@@ -863,7 +868,7 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
         resource(static_cast<uint8_t *>(what.out()) +
                      (what.out_row(held) * what.out_stride() + held.col) *
                          T::kBytes,
-                 Stream::TR * out_stride);
+                 Stream::TR * stride);
     const auto out = __builtin_amdgcn_make_buffer_rsrc(
         reinterpret_cast<void *>(uint64_t(words[1]) << 32 | words[0]), 0,
         words[2], words[3]);
@@ -872,8 +877,10 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
     for (int h = 0; h < 4; ++h)
       w[h] = pack_pair<T>(acc[f][2 * h][i], acc[f][2 * h + 1][i]);
     // dropped by the range check where there is no such row or column
-    const bool there = int(4 * quarter) < int(held.rows - row0) - 16 * f - i &&
-                       int(8 * p) < int(what.n_cols() - held.col - col0);
+    const uint32_t l = lane_again(), r = l >> 4 << 2, c = (l & 15) << 3;
+    const bool there = int(r) < int(held.rows - row0) - 16 * f - i &&
+                       int(c) < int(what.n_cols() - held.col - col0);
+    const uint32_t out_at = (row0 + r) * stride + (col0 + c) * T::kBytes;
     __builtin_amdgcn_raw_buffer_store_b128(w, out, there ? out_at : ~0u,
                                            (16 * f + i) * stride, 0);
   };
@@ -998,13 +1005,16 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
       if (last) break;
       if (kb + 1 == job.steps - 2) {
         tile += gridDim.x;
-        next = what.job(sums, tile, lane);
+        next = what.job(sums, tile, lane_again());
         aim(next);
         load_kb = 0;
       }
       block(std::false_type{}, even, job.start + kb + 2, load_kb++);
     }
-    held = job;
+    held.row = same(job.row);
+    held.rows = same(job.rows);
+    held.col = same(job.col);
+    held.expert = same(job.expert);
     job = next;
   } while (job.rows != 0);
 #pragma unroll
