@@ -472,8 +472,8 @@ __global__ void __launch_bounds__(256)
 // Rn and Cn are halves of the rows' and columns' fragments; each is read while the
 // quadrant before it is multiplied. One barrier a block, behind the last read of
 // its stage and the arrival of the next one. The results of a tile are stored
-// while the next tile's first block is multiplied: those of its upper half in front of
-// the first quadrant, which overwrites them, the others during the first two.
+// while the next tile's first block is multiplied: those of 16 rows in front of the
+// instructions that overwrite them, the lower half's during the second quadrant.
 struct Stream {
   static constexpr int TR = 256, TC = 256;
   static constexpr int kStage = (TR + TC) * 128;
@@ -847,7 +847,9 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
     constexpr int kNow = decltype(stage)::value;
 #pragma unroll
     for (int i = from; i < from + count; ++i) {
-      const int g = i / 4, f = i % 4;
+      // a tile's first quadrant by rows, whose last results have just been stored
+      const bool by_rows = decltype(first)::value && hr == 0 && hc == 0;
+      const int g = by_rows ? i % 4 : i / 4, f = by_rows ? i / 4 : i % 4;
       f32x4 &d = acc[4 * hr + f][4 * hc + g];
       const f32x4 zero = {0, 0, 0, 0};
       d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
@@ -859,30 +861,35 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
   };
   // the tile whose results are still in registers
   Job held{0, 0, 0, 0, 0, 0, 4};
-  const uint32_t out_stride = uint32_t(what.out_stride()) * T::kBytes;
-  // row 16 f + i of every 16 of the wave, eight columns a lane
-  const auto store = [&](int f, int i) {
-    uint32_t stride = out_stride;
-    asm volatile("" : "+s"(stride));  // what follows from it is not kept
+  // Where: rows that are not there fail the range check, as do all of a lane whose
+  // columns are not there.
+  struct Out {
+    __amdgpu_buffer_rsrc_t to;
+    uint32_t at, stride;
+  };
+  const auto aim_stores = [&] {
+    const uint32_t stride = uint32_t(what.out_stride()) * T::kBytes;
     const u32x4 words =
         resource(static_cast<uint8_t *>(what.out()) +
                      (what.out_row(held) * what.out_stride() + held.col) *
                          T::kBytes,
-                 Stream::TR * stride);
-    const auto out = __builtin_amdgcn_make_buffer_rsrc(
-        reinterpret_cast<void *>(uint64_t(words[1]) << 32 | words[0]), 0,
-        words[2], words[3]);
+                 held.rows * stride);
+    const uint32_t l = lane_again(), r = row0 + (l >> 4 << 2);
+    const uint32_t c = col0 + ((l & 15) << 3);
+    return Out{__builtin_amdgcn_make_buffer_rsrc(
+                   reinterpret_cast<void *>(uint64_t(words[1]) << 32 | words[0]),
+                   0, words[2], words[3]),
+               c < what.n_cols() - held.col ? r * stride + c * T::kBytes : ~0u,
+               stride};
+  };
+  // row 16 f + i of every 16 of the wave, eight columns a lane
+  const auto store = [&](const Out &out, int f, int i) {
     u32x4 w;
 #pragma unroll
     for (int h = 0; h < 4; ++h)
       w[h] = pack_pair<T>(acc[f][2 * h][i], acc[f][2 * h + 1][i]);
-    // dropped by the range check where there is no such row or column
-    const uint32_t l = lane_again(), r = l >> 4 << 2, c = (l & 15) << 3;
-    const bool there = int(r) < int(held.rows - row0) - 16 * f - i &&
-                       int(c) < int(what.n_cols() - held.col - col0);
-    const uint32_t out_at = (row0 + r) * stride + (col0 + c) * T::kBytes;
-    __builtin_amdgcn_raw_buffer_store_b128(w, out, there ? out_at : ~0u,
-                                           (16 * f + i) * stride, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(w, out.to, out.at,
+                                           (16 * f + i) * out.stride, 0);
   };
 
   // A block of the tile, in stage 0 or 1. It loads block load_kb of the tile that is
@@ -904,38 +911,38 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
     constexpr uint32_t kNow = decltype(stage)::value, kNext = kNow ^ 1;
     i32x8(&c0)[4] = cs[kNow];
     i32x8(&c1)[4] = cs[kNext];
-    // two rows' stores of the last tile's results
-    const auto old = [&](uint32_t n) {
+    // stores [from, from + count) of the last tile's results
+    Out out;
+    if constexpr (kFirst) out = aim_stores();
+    const auto old = [&](uint32_t from, uint32_t count) {
       if constexpr (kFirst) {
 #pragma unroll
-        for (uint32_t k = 2 * n; k < 2 * n + 2; ++k) {
-          store(k / 4, k % 4);
+        for (uint32_t k = from; k < from + count; ++k) {
+          store(out, k / 4, k % 4);
           in_order();
         }
       }
     };
     point(load_kb);
-    each([&](auto i) {
-      old(2 * i.value);
-      old(2 * i.value + 1);
-    });
+    old(0, 4);
     in_order();
     each([&](auto i) {
       c1[i.value] = read_col(4 + i.value, kNow);
       load_row(even, i, stage, load_kb);
       multiply(first, stage, 0, 0, r0, c0, 4 * i.value, 2);
       in_order();
+      old(4 * i.value + 4, 2);
       load_col(even, i, stage, load_kb);
       multiply(first, stage, 0, 0, r0, c0, 4 * i.value + 2, 2);
       in_order();
-      old(8 + i.value);
+      old(4 * i.value + 6, 2);
     });
     load_scales(stage, load_kb);
     each([&](auto i) {
       r1[i.value] = read_row(4 + i.value, kNow);
       multiply(first, stage, 0, 1, r0, c1, 2 * i.value, 2);
       in_order();
-      old(12 + i.value);
+      old(20 + 3 * i.value, 3);
     });
     multiply(first, stage, 0, 1, r0, c1, 8, 8);
     in_order();
@@ -1017,8 +1024,9 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
     held.expert = same(job.expert);
     job = next;
   } while (job.rows != 0);
+  const Out out = aim_stores();
 #pragma unroll
-  for (int k = 0; k < 32; ++k) store(k / 4, k % 4);
+  for (int k = 0; k < 32; ++k) store(out, k / 4, k % 4);
 }
 
 // Where an expert's columns start and how many there are, in blocks of 128
