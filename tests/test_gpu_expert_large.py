@@ -103,6 +103,32 @@ def test_rows_and_results_of_products(cl, dtype):
     assert (out[-301] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_weight_grad_past_the_caches(cl, dtype):
+    """Results of more than 256 MiB, of ragged tiles; no row twice alike."""
+    E, N, C = 19, 2600, 2824
+    counts = [(7 * e) % 13 * 20 for e in range(E)]
+    off = torch.tensor([0] + counts).cumsum(0).int()
+    P = int(off[-1])
+    g = torch.Generator().manual_seed(1)
+    dy = torch.randint(-2, 3, (P, N), generator=g).to(dtype)
+    x = torch.randint(-2, 3, (P, C), generator=g).to(dtype)
+    L = cl.ciera_columns_length(P, E)
+    S = -(-L // 512) * 4
+    yt, xt = zeros8(N, L), zeros8(C, L)
+    ys = torch.zeros(N, S, dtype=torch.uint8, device=DEV)
+    xs = torch.zeros(C, S, dtype=torch.uint8, device=DEV)
+    at = off.to(DEV)
+    cl.quantize_columns_t(dy.to(DEV), at, yt, ys)
+    cl.quantize_columns_t(x.to(DEV), at, xt, xs)
+    dw = torch.full((E, N, C), 7, dtype=dtype, device=DEV)
+    cl.expert_weight_grad_t(yt, ys, xt, xs, at, dw)
+    for e in range(E):
+        rows = slice(int(off[e]), int(off[e + 1]))
+        exact = dy[rows].float().t() @ x[rows].float()  # below 4 * 240
+        assert torch.equal(dw[e].cpu(), exact.to(dtype)), e
+
+
 def test_blocks(cl):
     E, N, C = 130, 4100, 8200  # 8.7 GB, 8 bits 4.4 GB each way
     w = torch.zeros(E, N, C, dtype=torch.bfloat16, device=DEV)
