@@ -324,13 +324,15 @@ def ciera_combine_backward(d_out, d_out_stride, rows, dtype, n_rows, n_cols,
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream():
-    """The current stream's handle. Asked for directly where torch has the call
-    for it: the Stream object that torch.cuda.current_stream() builds around it
-    costs 2.8 us a call, as much as a kernel launch; this takes 0.3."""
+def _stream(device=None):
+    """The current stream's handle; ``device`` is the current device's index
+    where it is known. Asked for directly where torch has the call for it: the
+    Stream object that torch.cuda.current_stream() builds around it costs 2.8
+    us a call, as much as a kernel launch; this takes 0.3."""
     if _raw_stream is None:
         return torch.cuda.current_stream().cuda_stream
-    return _raw_stream(torch.cuda.current_device())
+    return _raw_stream(torch.cuda.current_device() if device is None
+                       else device)
 
 
 def _ptr(t):
@@ -493,10 +495,18 @@ def _dims(t, name, n):
     return t.shape
 
 
-def _row_stride(t):
-    """Elements from a row of a checked matrix to the next."""
-    rows, cols = t.shape
-    return t.stride(0) if rows > 1 and cols > 0 else cols or 1
+def _refuse_dims(*args):
+    """Say which (tensor, name, dimensions) has others, after its shape did not
+    unpack; asked first, it would cost 0.2 us a tensor."""
+    for t, name, n in args:
+        _dims(t, name, n)
+    raise ValueError("arguments do not fit each other")
+
+
+def _row_stride(t, cols):
+    """Elements from a row of a checked matrix of ``cols`` columns to the next.
+    Asking a tensor for one stride costs four times what is_contiguous does."""
+    return (cols or 1) if t.is_contiguous() else t.stride(0)
 
 
 def _scales_fit(s, filled):
@@ -515,8 +525,10 @@ def route_t(logits, expert_ids, weights, bias=None, groups=1, top_groups=1,
             group_top_two=False, sigmoid=False, normalize=False, scale=1.0):
     """Choose experts: ``logits`` [T, E] -> ``expert_ids`` int32 and
     ``weights`` fp32, both [T, k]; ``bias`` fp32 [E]."""
-    T, E = _dims(logits, "logits", 2)
-    k = _dims(expert_ids, "expert_ids", 2)[1]
+    try:
+        (T, E), (_, k) = logits.shape, expert_ids.shape
+    except ValueError:
+        _refuse_dims((logits, "logits", 2), (expert_ids, "expert_ids", 2))
     dev = _device(logits, "logits")
     if not (_strided(logits, dev, _WIDE, (T, E)) and
             _packed(expert_ids, dev, _INT, (T, k)) and
@@ -529,18 +541,20 @@ def route_t(logits, expert_ids, weights, bias=None, groups=1, top_groups=1,
     flags = ((ROUTE_SIGMOID if sigmoid else 0) |
              (ROUTE_NORMALIZE if normalize else 0) |
              (ROUTE_GROUP_TOP_TWO if group_top_two else 0))
-    rc = ciera_route(logits.data_ptr(), _WIDE[logits.dtype], T, E,
-                     _row_stride(logits), _ptr(bias), groups, top_groups, k,
-                     flags, scale, expert_ids.data_ptr(), weights.data_ptr(),
-                     _stream())
+    rc = lib().ciera_route(
+        logits.data_ptr(), _WIDE[logits.dtype], T, E, _row_stride(logits, E),
+        _ptr(bias), groups, top_groups, k, flags, scale,
+        expert_ids.data_ptr(), weights.data_ptr(), _stream(dev))
     return _check("ciera_route", rc)
 
 
 def route_backward_t(logits, expert_ids, d_weights, d_logits, sigmoid=False,
                      normalize=False, scale=1.0):
     """Gradient of route_t's weights -> gradient of its logits."""
-    T, E = _dims(logits, "logits", 2)
-    k = _dims(expert_ids, "expert_ids", 2)[1]
+    try:
+        (T, E), (_, k) = logits.shape, expert_ids.shape
+    except ValueError:
+        _refuse_dims((logits, "logits", 2), (expert_ids, "expert_ids", 2))
     dev = _device(logits, "logits")
     same = (logits.dtype,)
     if not (_strided(logits, dev, _WIDE, (T, E)) and
@@ -553,11 +567,10 @@ def route_backward_t(logits, expert_ids, d_weights, d_logits, sigmoid=False,
                 (d_logits, "d_logits", same, (T, E), _strided))
     flags = ((ROUTE_SIGMOID if sigmoid else 0) |
              (ROUTE_NORMALIZE if normalize else 0))
-    rc = ciera_route_backward(logits.data_ptr(), _WIDE[logits.dtype], T, E,
-                              _row_stride(logits), k, flags, scale,
-                              expert_ids.data_ptr(), d_weights.data_ptr(),
-                              d_logits.data_ptr(), _row_stride(d_logits),
-                              _stream())
+    rc = lib().ciera_route_backward(
+        logits.data_ptr(), _WIDE[logits.dtype], T, E, _row_stride(logits, E),
+        k, flags, scale, expert_ids.data_ptr(), d_weights.data_ptr(),
+        d_logits.data_ptr(), _row_stride(d_logits, E), _stream(dev))
     return _check("ciera_route_backward", rc)
 
 
@@ -576,7 +589,10 @@ def route_plan_t(expert_ids, n_experts, offsets, source, position, ws,
                  first_expert=0):
     """Sort the (token, slot) pairs of ``expert_ids`` [T, k] by expert:
     ``offsets`` [n_experts + 1], ``source`` [T k], ``position`` [T, k]."""
-    T, k = _dims(expert_ids, "expert_ids", 2)
+    try:
+        T, k = expert_ids.shape
+    except ValueError:
+        _refuse_dims((expert_ids, "expert_ids", 2))
     dev = _device(expert_ids, "expert_ids")
     if not (_packed(expert_ids, dev, _INT, (T, k)) and
             _packed(offsets, dev, _INT, (n_experts + 1,)) and
@@ -588,10 +604,10 @@ def route_plan_t(expert_ids, n_experts, offsets, source, position, ws,
                 (source, "source", _INT, (T * k,), _packed),
                 (position, "position", _INT, (T, k), _packed),
                 (ws.buf, "the workspace", _BYTE, (ws.nbytes,), _packed))
-    rc = ciera_route_plan(expert_ids.data_ptr(), T, k, first_expert, n_experts,
-                          offsets.data_ptr(), source.data_ptr(),
-                          position.data_ptr(), ws.buf.data_ptr(), ws.nbytes,
-                          _stream())
+    rc = lib().ciera_route_plan(
+        expert_ids.data_ptr(), T, k, first_expert, n_experts,
+        offsets.data_ptr(), source.data_ptr(), position.data_ptr(),
+        ws.buf.data_ptr(), ws.nbytes, _stream(dev))
     return _check("ciera_route_plan", rc)
 
 
@@ -599,11 +615,15 @@ def quantize_rows_t(x, q, scales, position=None):
     """``x`` [R, C] -> 8-bit rows with a scale per 1 x 128 block: row r to row
     r, or with ``position`` [R, k] to the k rows that it names. ``q`` and
     ``scales`` have the shapes of quantized_shapes()."""
-    R, C = _dims(x, "x", 2)
-    Q = _dims(q, "q", 2)[0]
+    k = 1
+    try:
+        (R, C), (Q, _), (_, S) = x.shape, q.shape, scales.shape
+        if position is not None:
+            _, k = position.shape
+    except ValueError:
+        _refuse_dims((x, "x", 2), (q, "q", 2), (scales, "scales of q", 2),
+                     (position, "position", 2))
     filled = -(-C // 128) * 128
-    S = _dims(scales, "scales of q", 2)[1]
-    k = 1 if position is None else _dims(position, "position", 2)[1]
     dev = _device(x, "x")
     if not (_strided(x, dev, _WIDE, (R, C)) and
             _packed(q, dev, _E4M3, (Q, filled)) and
@@ -614,10 +634,9 @@ def quantize_rows_t(x, q, scales, position=None):
                 (q, "q", _E4M3, (Q, filled), _packed),
                 (scales, "scales of q", _BYTE, (Q, S), _packed),
                 (position, "position", _INT, (R, k), _packed))
-    rc = ciera_quantize_rows(x.data_ptr(), _WIDE[x.dtype], R, C,
-                             _row_stride(x), _ptr(position), k, Q,
-                             q.data_ptr(), filled, scales.data_ptr(), S,
-                             _stream())
+    rc = lib().ciera_quantize_rows(
+        x.data_ptr(), _WIDE[x.dtype], R, C, _row_stride(x, C), _ptr(position),
+        k, Q, q.data_ptr(), filled, scales.data_ptr(), S, _stream(dev))
     return _check("ciera_quantize_rows", rc)
 
 
@@ -645,10 +664,10 @@ def quantize_blocks_t(w, q, scales, q_t=None, scales_t=None):
                 (scales, "scales of q", _BYTE, (E, nb, S), _packed),
                 (q_t, "q_t", _E4M3, (E, C, 128 * nb), _packed),
                 (scales_t, "scales of q_t", _BYTE, (E, cb, St), _packed))
-    rc = ciera_quantize_blocks(w.data_ptr(), _WIDE[w.dtype], E, N, C,
-                               q.data_ptr(), 128 * cb, scales.data_ptr(), S,
-                               _ptr(q_t), 128 * nb, _ptr(scales_t), St,
-                               _stream())
+    rc = lib().ciera_quantize_blocks(
+        w.data_ptr(), _WIDE[w.dtype], E, N, C, q.data_ptr(), 128 * cb,
+        scales.data_ptr(), S, _ptr(q_t), 128 * nb, _ptr(scales_t), St,
+        _stream(dev))
     return _check("ciera_quantize_blocks", rc)
 
 
@@ -674,10 +693,10 @@ def quantize_columns_t(x, offsets, q_t, scales_t, source=None, top_k=1):
                 (q_t, "q_t", _E4M3, (C, L), _packed),
                 (scales_t, "scales of q_t", _BYTE, (C, S), _packed),
                 (source, "source", _INT, (P,), _packed))
-    rc = ciera_quantize_columns(x.data_ptr(), _WIDE[x.dtype], R, P, C,
-                                _row_stride(x), _ptr(source), top_k,
-                                offsets.data_ptr(), E, q_t.data_ptr(), L,
-                                scales_t.data_ptr(), S, _stream())
+    rc = lib().ciera_quantize_columns(
+        x.data_ptr(), _WIDE[x.dtype], R, P, C, _row_stride(x, C),
+        _ptr(source), top_k, offsets.data_ptr(), E, q_t.data_ptr(), L,
+        scales_t.data_ptr(), S, _stream(dev))
     return _check("ciera_quantize_columns", rc)
 
 
@@ -685,10 +704,13 @@ def expert_matmul_t(a, a_scales, b, b_scales, offsets, out):
     """8-bit rows ``a`` [P, D] times the 8-bit weights ``b`` [E, N, D] of their
     experts -> ``out`` [P, N]; ``offsets`` int32 [E + 1], or None for one
     expert."""
-    P, D = _dims(a, "a", 2)
-    E, N = _dims(b, "b", 3)[:2]
-    Sa = _dims(a_scales, "scales of a", 2)[1]
-    Sb = _dims(b_scales, "scales of b", 3)[2]
+    try:
+        (P, D), (E, N, _), (_, Sa), (_, _, Sb) = (a.shape, b.shape,
+                                                  a_scales.shape,
+                                                  b_scales.shape)
+    except ValueError:
+        _refuse_dims((a, "a", 2), (b, "b", 3), (a_scales, "scales of a", 2),
+                     (b_scales, "scales of b", 3))
     nb = -(-N // 128)
     dev = _device(a, "a")
     if not (_strided(a, dev, _E4M3, (P, D)) and
@@ -704,11 +726,11 @@ def expert_matmul_t(a, a_scales, b, b_scales, offsets, out):
                 (b_scales, "scales of b", _BYTE, (E, nb, Sb), _packed),
                 (out, "out", _WIDE, (P, N), _strided),
                 (offsets, "offsets", _INT, (E + 1,), _packed))
-    rc = ciera_expert_matmul(a.data_ptr(), _row_stride(a),
-                             a_scales.data_ptr(), _row_stride(a_scales), P,
-                             b.data_ptr(), D, b_scales.data_ptr(), Sb, E, N, D,
-                             _ptr(offsets), out.data_ptr(), _WIDE[out.dtype],
-                             _row_stride(out), _stream())
+    rc = lib().ciera_expert_matmul(
+        a.data_ptr(), _row_stride(a, D), a_scales.data_ptr(),
+        _row_stride(a_scales, Sa), P, b.data_ptr(), D, b_scales.data_ptr(),
+        Sb, E, N, D, _ptr(offsets), out.data_ptr(), _WIDE[out.dtype],
+        _row_stride(out, N), _stream(dev))
     return _check("ciera_expert_matmul", rc)
 
 
@@ -733,18 +755,20 @@ def expert_weight_grad_t(dy_t, dy_scales, x_t, x_scales, offsets, d_w):
                 (x_scales, "scales of x_t", _BYTE, (C, Sx), _packed),
                 (offsets, "offsets", _INT, (E + 1,), _packed),
                 (d_w, "d_w", _WIDE, (E, N, C), _packed))
-    rc = ciera_expert_weight_grad(dy_t.data_ptr(), dy_scales.data_ptr(), Sy,
-                                  x_t.data_ptr(), x_scales.data_ptr(), Sx, L,
-                                  E, N, C, offsets.data_ptr(), d_w.data_ptr(),
-                                  _WIDE[d_w.dtype], _stream())
+    rc = lib().ciera_expert_weight_grad(
+        dy_t.data_ptr(), dy_scales.data_ptr(), Sy, x_t.data_ptr(),
+        x_scales.data_ptr(), Sx, L, E, N, C, offsets.data_ptr(),
+        d_w.data_ptr(), _WIDE[d_w.dtype], _stream(dev))
     return _check("ciera_expert_weight_grad", rc)
 
 
 def combine_t(rows, position, out, weights=None):
     """``out`` [T, C]: for every token the sum of the rows [P, C] that
     ``position`` [T, k] names, times ``weights`` [T, k] if given."""
-    P, C = _dims(rows, "rows", 2)
-    T, k = _dims(position, "position", 2)
+    try:
+        (P, C), (T, k) = rows.shape, position.shape
+    except ValueError:
+        _refuse_dims((rows, "rows", 2), (position, "position", 2))
     dev = _device(rows, "rows")
     same = (rows.dtype,)
     if not (_strided(rows, dev, _WIDE, (P, C)) and
@@ -755,9 +779,10 @@ def combine_t(rows, position, out, weights=None):
                 (position, "position", _INT, (T, k), _packed),
                 (out, "out", same, (T, C), _strided),
                 (weights, "weights", _FLOAT, (T, k), _packed))
-    rc = ciera_combine(rows.data_ptr(), _WIDE[rows.dtype], P, C,
-                       _row_stride(rows), _ptr(weights), position.data_ptr(),
-                       T, k, out.data_ptr(), _row_stride(out), _stream())
+    rc = lib().ciera_combine(
+        rows.data_ptr(), _WIDE[rows.dtype], P, C, _row_stride(rows, C),
+        _ptr(weights), position.data_ptr(), T, k, out.data_ptr(),
+        _row_stride(out, C), _stream(dev))
     return _check("ciera_combine", rc)
 
 
@@ -779,9 +804,9 @@ def combine_backward_t(d_out, rows, weights, position, d_rows, d_weights):
                 (weights, "weights", _FLOAT, (T, k), _packed),
                 (d_rows, "d_rows", same, (P, C), _strided),
                 (d_weights, "d_weights", _FLOAT, (T, k), _packed))
-    rc = ciera_combine_backward(
-        d_out.data_ptr(), _row_stride(d_out), rows.data_ptr(),
-        _WIDE[rows.dtype], P, C, _row_stride(rows), weights.data_ptr(),
-        position.data_ptr(), T, k, d_rows.data_ptr(), _row_stride(d_rows),
-        d_weights.data_ptr(), _stream())
+    rc = lib().ciera_combine_backward(
+        d_out.data_ptr(), _row_stride(d_out, C), rows.data_ptr(),
+        _WIDE[rows.dtype], P, C, _row_stride(rows, C), weights.data_ptr(),
+        position.data_ptr(), T, k, d_rows.data_ptr(), _row_stride(d_rows, C),
+        d_weights.data_ptr(), _stream(dev))
     return _check("ciera_combine_backward", rc)

@@ -592,8 +592,8 @@ __device__ __forceinline__ uint32_t same(uint32_t x) {
 
 // What a stream multiplies: the order of its tiles and where their operands are.
 // Tiles in an order that the XCDs' caches like: the 32 workgroups of an XCD take 4
-// x 8 neighbours at a time (2 x 16: 896 us against 880 for 65,536 rows x 7168 x
-// 2048; workgroups in order: 903).
+// x 8 neighbours at a time (2 x 16: 836 us against 817 for 65,536 rows x 7168 x
+// 2048; workgroups in order: 841).
 struct ProductStream {
   MatmulArgs a;
   uint32_t row_tiles, col_tiles;
