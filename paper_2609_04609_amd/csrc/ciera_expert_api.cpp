@@ -105,7 +105,10 @@ uint64_t ciera_plan_workspace_bytes(uint64_t n_tokens, uint32_t top_k,
   if (n_experts == 0 || n_experts > CIERA_MAX_EXPERTS || top_k == 0 ||
       top_k > CIERA_MAX_TOP_K || n_tokens >= kMost || n_tokens * top_k >= kMost)
     return 0;
-  const uint64_t tiles = plan_tiles(n_tokens * top_k);
+  // enough for fewer pairs too, which smaller tiles may take
+  uint64_t tiles = plan_tiles(n_tokens * top_k);
+  if (n_tokens * top_k > kPlanSmall && tiles < plan_tiles(kPlanSmall))
+    tiles = plan_tiles(kPlanSmall);
   return ((tiles + 1) * n_experts * 4 + 255) & ~uint64_t(255);
 }
 

@@ -359,6 +359,22 @@ def test_plan(cl, T, k, E, first):
         assert torch.equal(pos.cpu().long(), p)
 
 
+@pytest.mark.parametrize("T,k,E", [(129, 2, 3), (1023, 2, 64), (1025, 2, 64),
+                                   (40_000, 3, 256), (70_001, 8, 65)])
+def test_plan_of_every_tile(cl, T, k, E):
+    """Few pairs shared by all waves, and both sizes of tiles."""
+    g = torch.Generator().manual_seed(T)
+    ids = torch.randint(-1, E + 1, (T, k), generator=g, dtype=torch.int32)
+    off = torch.full((E + 1,), -9, dtype=torch.int32, device=DEV)
+    src = torch.full((T * k,), -9, dtype=torch.int32, device=DEV)
+    pos = torch.full((T, k), -9, dtype=torch.int32, device=DEV)
+    cl.route_plan_t(ids.to(DEV), E, off, src, pos, cl.PlanWorkspace(T, k, E))
+    o, s, p = ref.plan(ids, E)
+    assert torch.equal(off.cpu().long(), o)
+    assert torch.equal(src.cpu().long(), s)
+    assert torch.equal(pos.cpu().long(), p)
+
+
 def test_route_and_plan_in_a_graph(cl):
     T, E, k = 300, 64, 8
     l = randn(T, E, seed=1).to(DEV)

@@ -188,6 +188,18 @@ def test_the_reference_itself():
     assert p.tolist() == [[1, 0], [-1, 2]]
 
 
+def test_plan_workspace_grows(cl):
+    """A workspace for some tokens is enough for fewer."""
+    for k, E in ((1, 3), (8, 64)):
+        last = 0
+        for n in sorted({0, 1, 100, 255, 256, 257, 2047, 2048, 2049, 65535,
+                         65536, 65537, 70000, 131072, 131073, 524287, 524288,
+                         524289, 600000, 1048576, 1048577, 1 << 24}):
+            need = cl.ciera_plan_workspace_bytes(n, k, E)
+            assert need >= last, (k, n)
+            last = need
+
+
 def test_launches_past_32_bits_of_threads(cl):
     """Sizes that a device's memory could hold but one launch could not cover."""
     big = 1 << 26
