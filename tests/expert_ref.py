@@ -16,10 +16,21 @@ def top_of(values, n):
 
 
 def scores(l, sigmoid):
-    """Softmax (of a row whose -inf entries are masked) or sigmoid."""
+    """Softmax (of a row whose -inf entries are masked) or sigmoid of a row, value
+    by value: torch's own may give equal logits scores that differ in the last
+    bit, by their place in the row."""
+    x = l.tolist()
+    top = max(x)
     if sigmoid:
-        return torch.sigmoid(l)
-    return torch.softmax(l, -1) if (l > -INF).any() else torch.zeros_like(l)
+        s = [1 / (1 + math.exp(-v)) if v > 0 else
+             math.exp(v) / (1 + math.exp(v)) for v in x]
+    elif top == -INF:
+        s = [0.0] * len(x)
+    else:
+        e = [math.exp(v - top) for v in x]
+        total = math.fsum(e)
+        s = [v / total for v in e]
+    return torch.tensor(s, dtype=torch.float64)
 
 
 def route(logits, k, bias=None, groups=1, top_groups=1, two=False,
