@@ -491,8 +491,9 @@ __global__ void __launch_bounds__(256)
 //   LDS reads  C1         R1        |         |  R0 of the next  C0 of the next
 //   loads                           | block two ahead, into the stage that is free
 // Rn and Cn are halves of the rows' and columns' fragments; each is read while the
-// quadrant before it is multiplied. One barrier a block, behind the last read of
-// its stage and the arrival of the next one. The results of a tile are stored
+// quadrant before it is multiplied. Two barriers a block, in its middle and at its
+// end, each behind the arrival of half of the next block and the last read of what
+// the loads behind it overwrite. The results of a tile are stored
 // while the next tile's first block is multiplied: those of 16 rows in front of the
 // instructions that overwrite them, the lower half's during the second quadrant.
 // Loads and stores end in order: what the first block loads ahead is asked for before
