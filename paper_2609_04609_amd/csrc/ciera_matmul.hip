@@ -1200,21 +1200,30 @@ hipError_t few_rows(const MatmulArgs &a, uint64_t experts, hipStream_t s) {
 //                           200       100           70           73
 // Tiles cost a round of the CUs for every 256 of them, 1.6 us a block of the depth.
 // few_rows reads the weights anew for every 16 or 64 rows of an expert, at 4 and 1.6 TB/s
-// with what else it does; an expert's last rows fill half of such a group. fp32 results
-// take tiles twice as long. With a row or two an expert the weights' own bytes are all.
-int few_fragments(const MatmulArgs &a, uint64_t experts, bool fp32) {
+// with what else it does (fp32 results 2.8 and 1.2); an expert's last rows fill half of
+// such a group. Results that do not stream and fill few tiles of 256 take tiles of 128, a
+// block of 256 of which costs 1.15 us, fp32 results 1.4 (large tiles 3.1): 10,584
+// rows of 64 x 170 x 3968 in fp32 44 us, with 4 fragments 119; 9396 rows of 4 x 127 x
+// 3200 in bf16 29 us and 48. With a row or two an expert the weights' own bytes are all.
+int few_fragments(const MatmulArgs &a, uint64_t experts, bool fp32,
+                  bool streams) {
   if (a.n_rows <= 2 * experts) return 1;
   const auto groups = [&](uint64_t of) {
     const uint64_t g = a.n_rows / of + experts / 2;
     return double(g > experts ? g : experts);
   };
   const double weight = double(a.n_out) * double(a.depth);
-  const double rounds = std::ceil(
-      groups(256) * std::ceil(double(a.n_out) / 256) / kStreamGroups);
-  const double tiles =
-      6 + rounds * double(a.depth / 128) * (fp32 ? 3.2 : 1.6);
-  const double one = groups(16) * weight / 4.0e6;
-  const double four = groups(64) * weight / 1.6e6;
+  const double blocks = double(a.depth / 128);
+  double tiles = 6;
+  if (streams || many_tiles(a.n_rows, a.n_out)) {
+    tiles += std::ceil(groups(256) * std::ceil(double(a.n_out) / 256) /
+                       kStreamGroups) * blocks * (fp32 ? 3.1 : 1.6);
+  } else {
+    const double of_cus = groups(128) * std::ceil(double(a.n_out) / 128) / 256;
+    tiles += (of_cus > 1 ? of_cus : 1) * blocks * (fp32 ? 1.4 : 1.15);
+  }
+  const double one = groups(16) * weight / (fp32 ? 2.8e6 : 4.0e6);
+  const double four = groups(64) * weight / (fp32 ? 1.2e6 : 1.6e6);
   if (one <= four && one < tiles) return 1;
   return four < tiles ? 4 : 0;
 }
@@ -1223,13 +1232,15 @@ template <typename T>
 hipError_t matmul_typed(const MatmulArgs &a, hipStream_t s) {
   const uint64_t experts =
       !a.offsets ? 1 : a.n_rows < a.n_experts ? a.n_rows : a.n_experts;
-  const int few = few_fragments(a, experts, T::kBytes == 4);
+  const bool streams =
+      T::kBytes == 2 && a.depth >= 512 &&
+      stream_fits(a.a_stride, a.b_stride, a.a_scale_stride, a.b_scale_stride,
+                  a.out, a.out_stride, a.n_out);
+  const int few = few_fragments(a, experts, T::kBytes == 4, streams);
   if (few == 1) return few_rows<T, 1>(a, experts, s);
   if (few == 4) return few_rows<T, 4>(a, experts, s);
   if constexpr (T::kBytes == 2) {
-    if (a.depth >= 512 &&
-        stream_fits(a.a_stride, a.b_stride, a.a_scale_stride,
-                    a.b_scale_stride, a.out, a.out_stride, a.n_out)) {
+    if (streams) {
       const ProductStream what{
           a, uint32_t((a.n_rows + (Stream::TR - 1) * experts) / Stream::TR),
           uint32_t((a.n_out + Stream::TC - 1) / Stream::TC)};
