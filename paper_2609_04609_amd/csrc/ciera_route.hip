@@ -145,15 +145,15 @@ __device__ __forceinline__ O team_lane(O x, uint32_t i) {
 }
 
 // Whether groups of S experts are whole lanes of a row, 1, 2, 4 ... 16 of them.
-__host__ __device__ inline bool groups_in_row(uint32_t S, uint32_t V) {
+__device__ inline bool groups_in_row(uint32_t S, uint32_t V) {
   const uint32_t lanes = S / V;
   return S % V == 0 && (lanes & (lanes - 1)) == 0 && lanes <= 16;
 }
 
 // Keep the top_groups groups of highest rank; the keys of others become 0.
 // Returns whether the border between them is closer than K tells apart. Groups
-// in a row are reduced there; others, for teams of 64, go through `shared`, 64 V
-// keys of this wave, a lane a group.
+// in a row are reduced there, as are all of whole lanes for teams of 16; others, for
+// teams of 64, go through `shared`, 64 V keys of this wave, a lane a group.
 template <typename K, int V, int L>
 __device__ __forceinline__ bool choose_groups(const RouteArgs &a,
                                               Order<K> (&key)[V], uint32_t lane,
@@ -164,7 +164,16 @@ __device__ __forceinline__ bool choose_groups(const RouteArgs &a,
   const uint32_t lanes = S / V;
   const bool in_row = L == 16 || groups_in_row(S, V);
   O one = 0, two = 0;
-  if (in_row) {
+  if (L == 16 && (lanes & (lanes - 1)) != 0) {
+    // of another number of lanes of a team of 16: one after the other
+    O mine_one = key[0], mine_two = 0;
+#pragma unroll
+    for (int j = 1; j < V; ++j) merge_two(mine_one, mine_two, key[j], O(0));
+    const uint32_t from = lane / lanes * lanes;
+    for (uint32_t i = 0; i < lanes; ++i)
+      merge_two(one, two, team_lane<L>(mine_one, from + i),
+                team_lane<L>(mine_two, from + i));
+  } else if (in_row) {
     one = key[0];
 #pragma unroll
     for (int j = 1; j < V; ++j) merge_two(one, two, key[j], O(0));
@@ -725,8 +734,7 @@ hipError_t route_wide(const RouteArgs &a, hipStream_t s) {
 // Whether V experts a lane in teams of 16 hold the tokens.
 bool in_rows(const RouteArgs &a, uint32_t V) {
   return a.n_experts <= 16 * V && a.top_k <= 16 && a.n_tokens >= kRowTokens &&
-         (a.top_groups == a.n_groups ||
-          groups_in_row(a.n_experts / a.n_groups, V));
+         (a.top_groups == a.n_groups || a.n_experts / a.n_groups % V == 0);
 }
 template <typename T>
 hipError_t route_typed(const RouteArgs &a, hipStream_t s) {

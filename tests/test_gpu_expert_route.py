@@ -177,7 +177,9 @@ def check_many(cl, rows, k, **o):
     (torch.float32, 64, 8, 16, 5, True), (torch.bfloat16, 100, 17, 1, 1, False),
     (torch.float32, 128, 16, 2, 1, True), (torch.float16, 130, 3, 1, 1, True),
     (torch.float32, 256, 8, 8, 4, True), (torch.float32, 256, 16, 16, 9, False),
-    (torch.bfloat16, 252, 4, 12, 5, True), (torch.bfloat16, 257, 8, 1, 1, False)])
+    (torch.bfloat16, 252, 4, 12, 5, True), (torch.bfloat16, 257, 8, 1, 1, False),
+    (torch.float32, 160, 4, 2, 1, True), (torch.bfloat16, 192, 7, 4, 2, False),
+    (torch.float16, 24, 3, 2, 1, True), (torch.float32, 240, 16, 3, 2, True)])
 def test_many_tokens(cl, o, dtype, E, k, G, t, two):
     rows = randn(29, E, seed=E + k, std=2.0)
     if E > 8:
