@@ -680,7 +680,8 @@ struct GradStream {
   static constexpr bool kColBlocks = false;
   __device__ __forceinline__ uint32_t n_cols() const { return uint32_t(a.n_cols); }
   __device__ __forceinline__ void prepare(Sums &s, uint32_t lane) const {
-    sum_experts(s, a.offsets, a.n_experts, ~0u, 7, lane);
+    // no expert has more rows than there are columns
+    sum_experts(s, a.offsets, a.n_experts, uint32_t(a.length), 7, lane);
   }
   __device__ __forceinline__ Job job(const Sums &s, uint32_t t, uint32_t) const {
     Job j{0, 0, 0, 0, 0, 0, 4};
@@ -697,7 +698,10 @@ struct GradStream {
     const uint32_t start = same(s.before[j.expert]);
     const uint32_t end = same(s.before[j.expert + 1]);
     j.start = start < most ? start : most;
-    j.real = (end < most ? end : most) - j.start;
+    // offsets that rise and fall can pass 2^32 in the sums, so the end need not lie
+    // behind the start
+    const uint32_t last = end < most ? end : most;
+    j.real = last > j.start ? last - j.start : 0;
     j.steps = padded_steps(j.real);
     return j;
   }
@@ -1073,20 +1077,21 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
 // Where an expert's columns start and how many there are, in blocks of 128
 // rows.
 __device__ __forceinline__ void blocks_of_expert(const int32_t *offsets,
+                                                 uint32_t n_rows,
                                                  uint32_t expert, uint32_t lane,
                                                  uint32_t &start,
                                                  uint32_t &blocks) {
   uint32_t sum = 0;
   for (uint32_t e = lane; e < expert; e += 64) {
-    const uint32_t lo = offset_of(offsets, e, ~0u);
-    const uint32_t hi = offset_of(offsets, e + 1, ~0u);
+    const uint32_t lo = offset_of(offsets, e, n_rows);
+    const uint32_t hi = offset_of(offsets, e + 1, n_rows);
     sum += hi > lo ? (hi - lo + 127) / 128 : 0;
   }
   uint32_t total;
   wave_prefix(sum, total);
   start = total;
-  const uint32_t lo = offset_of(offsets, expert, ~0u);
-  const uint32_t hi = offset_of(offsets, expert + 1, ~0u);
+  const uint32_t lo = offset_of(offsets, expert, n_rows);
+  const uint32_t hi = offset_of(offsets, expert + 1, n_rows);
   blocks = hi > lo ? (hi - lo + 127) / 128 : 0;
 }
 
@@ -1103,7 +1108,7 @@ __global__ void __launch_bounds__(S::kThreads)
     return;
   const uint32_t row = row_tile * S::TR, col = at.col * S::TC;
   uint32_t start, blocks;
-  blocks_of_expert(a.offsets, expert, lane, start, blocks);
+  blocks_of_expert(a.offsets, uint32_t(a.length), expert, lane, start, blocks);
   const uint32_t most = uint32_t(a.length / 128);
   if (start > most) start = most;
   if (blocks > most - start) blocks = most - start;
