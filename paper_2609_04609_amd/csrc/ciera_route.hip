@@ -454,7 +454,8 @@ __global__ void __launch_bounds__(64 * kWaves)
 //   sigmoid normalised   d_i = w_i (1 - s_i) (g_i - sum_j w_j g_j / c)
 //   sigmoid              d_i = c s_i (1 - s_i) g_i
 // (d_i for the chosen; 0 elsewhere). Only the plain softmax reads the whole
-// row.
+// row. 1 - s is computed as the sigmoid of -l: subtracted from 1, an s close to it
+// leaves nothing (l = 16: 6% off, from 17 on 0).
 template <typename T, int V, int L>
 __global__ void __launch_bounds__(64 * kWaves)
     route_backward_kernel(RouteBackArgs a, bool vec, bool vec_out) {
@@ -499,16 +500,18 @@ __global__ void __launch_bounds__(64 * kWaves)
   } else if (normal) {
     const float high = from_order(team_max<L>(to_order(mine)));
     const bool as_exp = !sigmoid || high <= -30.0f;
-    const float s = sigmoid ? 1.0f / (1.0f + expf(-mine)) : 0.0f;
+    const float rest = sigmoid ? 1.0f / (1.0f + expf(mine)) : 1.0f;  // 1 - s
     float p = 0;
-    if (chosen && high != -kInf) p = as_exp ? expf(mine - high) : s;
+    if (chosen && high != -kInf)
+      p = as_exp ? expf(mine - high) : 1.0f / (1.0f + expf(-mine));
     const float all = team_sum<L>(p);
     const float w = all == 0 ? 0.0f : p / all;
     const float mean = team_sum<L>(chosen ? w * g : 0.0f);
-    d = chosen ? w * (1.0f - s) * (g - mean) : 0.0f;
+    d = chosen ? w * rest * (g - mean) : 0.0f;
   } else {
     const float s = 1.0f / (1.0f + expf(-mine));
-    d = chosen ? s * (1.0f - s) * g : 0.0f;
+    const float rest = 1.0f / (1.0f + expf(mine));  // 1 - s
+    d = chosen ? s * rest * g : 0.0f;
   }
   float o[V];
 #pragma unroll

@@ -54,3 +54,38 @@ def test_weight_grad_of_offsets_that_fall(cl, dtype, E, top):
         expect = dy[:, a:b] @ x[:, a:b].t()  # whole numbers below 2^14
         assert torch.equal(dw[e].cpu(), expect.to(dtype)), e
         start += n
+
+
+# ------------------------------------------------------- saturated scores ----
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16,
+                                   torch.float32])
+@pytest.mark.parametrize("times", [1, 90])  # 90: several tokens share a wave
+@pytest.mark.parametrize("normalize", [False, True])
+def test_gradient_of_saturated_sigmoids(cl, dtype, times, normalize):
+    """c s (1 - s) g relative to its own size, for logits of -30 to 30. s and 1 - s
+    are each an exponential (its argument is the logit itself; 1 ulp), a sum and a
+    division (2.5 ulp at most): 4 ulps of 2^-23. Scale, two products: 1.5 more. Two
+    chosen logits that are equal have weights of a half each (their scores are
+    the same number) and, with gradients g and -g, a mean of 0."""
+    l = torch.linspace(-30, 30, 61).to(dtype).view(-1, 1).repeat(times, 2)
+    T = l.shape[0]
+    k = 2 if normalize else 1
+    ids = torch.arange(k, dtype=torch.int32).repeat(T, 1)
+    g = randn(T, 1, seed=1)
+    dw = torch.cat([g, -g], 1)[:, :k].contiguous()
+    d = torch.full((T, 2), 7.0, dtype=dtype, device=DEV)
+    cl.route_backward_t(l.to(DEV), ids.to(DEV), dw.to(DEV), d, sigmoid=True,
+                        normalize=normalize, scale=2.5)
+    x, g = l[:, 0].double(), 2.5 * g[:, 0].double()
+    rest = 1 / (1 + torch.exp(x))
+    exact = rest * g * (0.5 if normalize else 1 / (1 + torch.exp(-x)))
+    bound = exact.abs() * (9.5 * 2.0 ** -23 + torch.finfo(dtype).eps / 2)
+    if dtype == torch.float16:
+        bound = bound + 2.0 ** -25  # half a step of its subnormal values
+    d = d.double().cpu()
+    assert ((d[:, 0] - exact).abs() <= bound).all()
+    if normalize:
+        assert ((d[:, 1] + exact).abs() <= bound).all()
+    else:
+        assert (d[:, 1] == 0).all()
