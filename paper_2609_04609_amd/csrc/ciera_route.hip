@@ -475,7 +475,10 @@ __global__ void __launch_bounds__(64 * kWaves)
     g = a.d_weights[uint64_t(token) * a.top_k + lane] * a.scale;
   }
   const bool chosen = uint32_t(id) < a.n_experts;
-  if (!chosen) id = -1;
+  if (!chosen) {  // adds nothing, whatever its gradient is
+    id = -1;
+    g = 0;
+  }
   const float mine = chosen ? T::to_float(row[id]) : -kInf;
   float d = 0;  // of this lane's slot
   float l[V], spread = 0, top = 0, sum = 1;

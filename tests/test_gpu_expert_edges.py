@@ -89,3 +89,27 @@ def test_gradient_of_saturated_sigmoids(cl, dtype, times, normalize):
         assert ((d[:, 1] + exact).abs() <= bound).all()
     else:
         assert (d[:, 1] == 0).all()
+
+
+@pytest.mark.parametrize("times", [1, 1100])  # 1100: several tokens share a wave
+@pytest.mark.parametrize("o", [dict(), dict(normalize=True),
+                               dict(sigmoid=True),
+                               dict(sigmoid=True, normalize=True)])
+def test_gradient_of_slots_without_an_expert(cl, o, times):
+    """Slots whose id is out of range add nothing, whatever their weight's gradient
+    is: the bits are those of gradients of 0 there."""
+    E, k = 20, 4
+    l = randn(4, E, seed=1).repeat(times, 1).to(DEV)
+    ids = torch.tensor([[3, -1, 7, 20], [-1, -1, -1, -1], [0, 19, -5, 2],
+                        [1, 2, 3, 4]], dtype=torch.int32)
+    dw = randn(4, k, seed=2)
+    clean = torch.where((ids >= 0) & (ids < E), dw, torch.zeros(4, k))
+    for bad in (math.nan, math.inf, -math.inf):
+        got = []
+        for g in (torch.where(clean == 0, torch.full_like(dw, bad), dw), clean):
+            d = torch.full_like(l, 7.0)
+            cl.route_backward_t(l, ids.repeat(times, 1).to(DEV),
+                                g.repeat(times, 1).to(DEV), d, **o)
+            got.append(d)
+        assert torch.isfinite(got[0]).all()
+        assert torch.equal(got[0], got[1])
