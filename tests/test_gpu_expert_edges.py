@@ -113,3 +113,69 @@ def test_gradient_of_slots_without_an_expert(cl, o, times):
             got.append(d)
         assert torch.isfinite(got[0]).all()
         assert torch.equal(got[0], got[1])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16,
+                                   torch.float32])
+@pytest.mark.parametrize("times", [1, 110])  # 110: several tokens share a wave
+@pytest.mark.parametrize("o", [dict(), dict(normalize=True),
+                               dict(sigmoid=True, normalize=True)])
+def test_gradient_of_saturated_weights(cl, dtype, times, o):
+    """One score of nearly 1, by a logit of 0 to 40 above the others, relative to the
+    gradients' own size. An exponential is off by 1 ulp of 2^-23, a sum of the seven
+    others by 3 more, of all by half, a division by 2.5: a score by 8 ulps, the
+    others' share by 11. 1 - s of a sigmoid is off by 4. The slots' gradients have
+    opposite signs, so that no difference between them is smaller than they are, and
+    the mean's error is at most its 9 ulps: with products and the scale 40 in all."""
+    E, scale = 8, 2.5
+    t = torch.arange(41).double().repeat(times)
+    T = t.numel()
+    l = torch.zeros(T, E, dtype=torch.float64)
+    l[:, 5] = t  # whole numbers to 40, which every type holds
+    k = 2 if o.get("normalize") else 1
+    ids = torch.tensor([5, 2][:k], dtype=torch.int32).repeat(T, 1)
+    a, b = randn(T, 1, seed=1).abs() + 0.1, -randn(T, 1, seed=2).abs() - 0.1
+    dw = torch.cat([a, b], 1)[:, :k].contiguous()
+    d = torch.full((T, E), 7.0, dtype=dtype, device=DEV)
+    cl.route_backward_t(l.to(dtype).to(DEV), ids.to(DEV), dw.to(DEV), d,
+                        scale=scale, **o)
+    a, b = scale * a[:, 0].double(), scale * b[:, 0].double()
+    exact = torch.zeros(T, E, dtype=torch.float64)
+    if not o:
+        p = 1 / (1 + 7 * torch.exp(-t))
+        q = torch.exp(-t) * p
+        exact[:] = (-q * p * a).unsqueeze(1)
+        exact[:, 5] = p * 7 * q * a
+    else:
+        s, r = 1 / (1 + torch.exp(-t)), 1 / (1 + torch.exp(t))
+        if o.get("sigmoid"):
+            w = 0.5 / (s + 0.5)  # the other's score is 1/2
+            exact[:, 5] = (1 - w) * r * w * (a - b)
+            exact[:, 2] = -w * 0.5 * (1 - w) * (a - b)
+        else:
+            exact[:, 5] = s * r * (a - b)
+            exact[:, 2] = -exact[:, 5]
+    bound = exact.abs() * (40 * 2.0 ** -23 + torch.finfo(dtype).eps / 2)
+    if dtype == torch.float16:
+        bound = bound + 2.0 ** -25  # half a step of its subnormal values
+    assert ((d.double().cpu() - exact).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("times", [1, 1500])
+@pytest.mark.parametrize("o", [dict(), dict(normalize=True)])
+def test_gradient_of_the_largest_score_named_twice(cl, o, times):
+    """Twice in the slots, or equal to another's, or with every score chosen: the
+    derivative in 64 bits, off by some 20 ulps of the largest term."""
+    l = torch.tensor([[9.0, 1.0, 0.0, 2.0], [3.0, 3.0, 3.0, -1.0],
+                      [-math.inf, 5.0, -math.inf, 5.0]])
+    ids = torch.tensor([[0, 0, 2, 0], [1, 0, 1, 3], [3, 1, 3, 1]])
+    dw = randn(3, 4, seed=4)
+    d = torch.full((3 * times, 4), 7.0, device=DEV)
+    cl.route_backward_t(l.repeat(times, 1).to(DEV),
+                        ids.int().repeat(times, 1).to(DEV),
+                        dw.repeat(times, 1).to(DEV), d, **o)
+    x = l.double().clamp(min=-2000).requires_grad_()
+    (ref.weights_of(x, ids, False, o.get("normalize", False), 1.0) *
+     dw.double()).sum().backward()
+    bound = 4 * 20 * 2.0 ** -23 * float(dw.abs().max())
+    assert ((d.double().cpu() - x.grad.repeat(times, 1)).abs() <= bound).all()
