@@ -33,6 +33,17 @@ def _shape(t, name, *shape):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, not {shape}")
 
 
+def _inputs(*args):
+    """Check (tensor, name, types, shape) of rows that may be apart, so that a
+    call refuses them before its first operator runs."""
+    for t, name, _, shape in args:
+        _shape(t, name, *shape)
+    dev = ciera._device(args[0][0], args[0][1])
+    if not all(ciera._strided(t, dev, types, shape)
+               for t, _, types, shape in args):
+        ciera._refuse(dev, *(a + (ciera._strided,) for a in args))
+
+
 class ExpertLayer:
     """``top_k`` of ``n_experts`` experts of [n_out, n_in] weights for
     ``n_tokens`` tokens of ``dtype``; ``choice`` are the keywords of
@@ -79,7 +90,12 @@ class ExpertLayer:
         (_, _), (_, Ls) = ciera.quantized_shapes(1, L)
         self.dy_t, self.dy_t_scales = eight(N, L), scales(N, Ls)
         self.x_t, self.x_t_scales = eight(C, L), scales(C, Ls)
-        self.d_w, self.d_logits = new(E, N, C), new(T, E)
+        self.d_w = new(E, N, C)
+        # the logits' gradient has their type, which need not be the tokens'
+        room = new(T * E, dtype=f32)
+        self._d_logits = {t: room.view(t)[:T * E].view(T, E)
+                          for t in (torch.bfloat16, torch.float16, f32)}
+        self.d_logits = self._d_logits[dtype]
 
     def load(self, w):
         """Take the weights ``w`` [n_experts, n_out, n_in]."""
@@ -89,9 +105,10 @@ class ExpertLayer:
 
     def forward(self, x, logits, bias=None):
         """``x`` [n_tokens, n_in] and the router's ``logits`` [n_tokens,
-        n_experts] -> the layer's output, [n_tokens, n_out]."""
-        _shape(x, "x", self.T, self.C)
-        _shape(logits, "logits", self.T, self.E)
+        n_experts], each of any wide type -> the layer's output, [n_tokens,
+        n_out]."""
+        _inputs((x, "x", ciera._WIDE, (self.T, self.C)),
+                (logits, "logits", ciera._WIDE, (self.T, self.E)))
         ciera.route_t(logits, self.ids, self.weights, bias, **self.choice)
         ciera.route_plan_t(self.ids, self.E, self.offsets, self.source,
                            self.position, self.ws)
@@ -103,12 +120,14 @@ class ExpertLayer:
 
     def backward(self, d_out, x, logits):
         """Gradient of the output that forward() gave for ``x`` and ``logits``
-        -> gradients of x, of the weights and of the logits."""
+        -> gradients of x, of the weights and of the logits, the first two of the
+        layer's type, the last of the logits'."""
         if not self.train:
             raise ValueError("a layer without train has no backward")
-        _shape(d_out, "d_out", self.T, self.N)
-        _shape(x, "x", self.T, self.C)
-        _shape(logits, "logits", self.T, self.E)
+        _inputs((d_out, "d_out", (self.out.dtype,), (self.T, self.N)),
+                (x, "x", ciera._WIDE, (self.T, self.C)),
+                (logits, "logits", ciera._WIDE, (self.T, self.E)))
+        self.d_logits = self._d_logits[logits.dtype]
         ciera.combine_backward_t(d_out, self.rows, self.weights,
                                  self.position, self.d_rows, self.d_weights)
         ciera.quantize_rows_t(self.d_rows, self.dy, self.dy_scales)

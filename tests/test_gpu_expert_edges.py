@@ -179,3 +179,77 @@ def test_gradient_of_the_largest_score_named_twice(cl, o, times):
      dw.double()).sum().backward()
     bound = 4 * 20 * 2.0 ** -23 * float(dw.abs().max())
     assert ((d.double().cpu() - x.grad.repeat(times, 1)).abs() <= bound).all()
+
+
+# ------------------------------------------------------- the layer's inputs ----
+
+def layer(*args, **o):
+    from paper_2609_04609_amd.experts import ExpertLayer
+    return ExpertLayer(*args, **o)
+
+
+@pytest.mark.parametrize("dtype,other", [
+    (torch.bfloat16, torch.float32), (torch.bfloat16, torch.float16),
+    (torch.float16, torch.float32), (torch.float32, torch.bfloat16)])
+def test_layer_with_logits_of_another_type(cl, dtype, other):
+    """A router in fp32 beside 16-bit tokens, and others. With logits that both types
+    hold everything has the bits of logits of the layer's type, and the
+    logits' gradient is the same fp32 number, rounded to their type."""
+    T, k, E, N, C = 70, 3, 12, 64, 136
+    m = layer(T, k, E, N, C, dtype=dtype, sigmoid=True, normalize=True)
+    m.load(randn(E, N, C, seed=1).to(dtype).to(DEV))
+    x, g = (randn(T, n, seed=n).to(dtype).to(DEV) for n in (C, N))
+    l = (randn(T, E, seed=3) * 64).round() / 64  # some 8 bits
+    l = l.to(torch.bfloat16).to(torch.float16)
+    runs = []
+    for t in (other, dtype, other):
+        y = m.forward(x, l.to(t).to(DEV))
+        grads = m.backward(g, x, l.to(t).to(DEV))
+        assert grads[2].dtype == t and grads[2] is m.d_logits
+        runs.append([v.clone() for v in (y,) + grads])
+    for a, b in zip(runs[0], runs[2]):
+        assert torch.equal(a, b)
+    for a, b in zip(runs[0][:3], runs[1][:3]):
+        assert torch.equal(a, b)
+    a, b = runs[0][3], runs[1][3]
+    wide, narrow = (a, b) if a.dtype == torch.float32 else (b, a)
+    if torch.float32 in (dtype, other):
+        assert torch.equal(wide.to(narrow.dtype), narrow)
+    assert float(a.float().abs().sum()) > 0
+
+
+def test_layer_refuses_before_it_runs(cl):
+    """An input that an operator in the middle of a call would refuse leaves the
+    layer's buffers as they were."""
+    T, k, E, N, C = 9, 2, 4, 40, 50
+    m = layer(T, k, E, N, C)
+    m.load(randn(E, N, C, seed=1).bfloat16().to(DEV))
+    x, g = (randn(T, n, seed=n).bfloat16().to(DEV) for n in (C, N))
+    l = randn(T, E, seed=3).to(DEV)
+    y = m.forward(x, l)
+    m.backward(g, x, l)
+    kept = [m.ids, m.weights, m.position, m.x, m.out, m.d_rows, m.d_weights,
+            m.d_x, m.d_w, m.d_logits]
+    before = [t.view(torch.uint8).clone() if t.dtype == E4M3 else t.clone()
+              for t in kept]
+    new = randn(T, E, seed=4).to(DEV)
+    bad = [
+        ("x has type", lambda: m.forward(x.int(), new)),
+        ("x is on cpu", lambda: m.forward(x.cpu(), new)),
+        ("x is not contiguous", lambda: m.forward(x.t().contiguous().t(), new)),
+        ("logits has type", lambda: m.forward(x, new.double())),
+        ("d_out has type", lambda: m.backward(g.float(), x, new)),
+        ("x has type", lambda: m.backward(2 * g, x.double(), new)),
+        ("logits has type", lambda: m.backward(2 * g, x, new.double())),
+        ("logits is on cpu", lambda: m.backward(2 * g, x, new.cpu())),
+        ("logits is not contiguous",
+         lambda: m.backward(2 * g, x, new.t().contiguous().t())),
+    ]
+    for what, call in bad:
+        with pytest.raises(ValueError, match=what):
+            call()
+    torch.cuda.synchronize()
+    for t, b in zip(kept, before):
+        t = t.view(torch.uint8) if t.dtype == E4M3 else t
+        assert torch.equal(t, b)
+    assert m.out is y
