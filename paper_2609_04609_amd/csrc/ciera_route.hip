@@ -106,10 +106,10 @@ __device__ __forceinline__ void merge_two(O &one, O &two, O other_one,
 // Whether neighbours in the order, values of K that are each within tol_abs +
 // tol_rel |value| of what they stand for, could stand in the other order.
 template <typename K>
-__device__ __forceinline__ bool too_close(K above, K below, float parts,
-                                          float tol_abs, float tol_rel) {
+__device__ __forceinline__ bool too_close(K above, K below, float tol_abs,
+                                          float tol_rel) {
   const K size = larger(larger(above, -above), larger(below, -below));
-  return above - below <= 2 * parts * (tol_abs + tol_rel * size);
+  return above - below <= 2 * (tol_abs + tol_rel * size);
 }
 
 // A team of L lanes, 64 or 16 (a row), holds a token; `lane` counts in the team.
@@ -205,7 +205,8 @@ __device__ __forceinline__ bool choose_groups(const RouteArgs &a,
         merge_two(one, two, shared[lane * S + i], O(0));
   }
   O rank_by = one;
-  if ((a.flags & CIERA_ROUTE_GROUP_TOP_TWO) && two != 0)
+  const bool two_values = a.flags & CIERA_ROUTE_GROUP_TOP_TWO;
+  if (two_values && two != 0)
     rank_by = to_order(from_order(one) + from_order(two));
   // group g's rank is in lane g * step
   const uint32_t step = in_row ? lanes : 1, mine = lane / step;
@@ -228,11 +229,19 @@ __device__ __forceinline__ bool choose_groups(const RouteArgs &a,
     }
   }
   if (!inexact) return false;
-  const O least = ~team_max<L>(kept ? O(~rank_by) : O(0));
-  const O most = team_max<L>(mine < a.n_groups && !kept ? rank_by : O(0));
-  // a group's rank has up to two values' errors
-  return most != 0 && too_close(K(from_order(least)), K(from_order(most)), 2,
-                                tol_abs, tol_rel);
+  // A rank is off by its values' errors, each relative to that value (they may cancel
+  // in the sum), and its own rounding. `off` is twice that, which covers the rounding of
+  // the rank's ends; where it is no number nothing is sure.
+  const bool sum = two_values && two != 0, live = one != 0;
+  const K f1 = from_order(one), f2 = sum ? from_order(two) : K(0);
+  const K off = 2 * ((sum ? 2 : 1) * K(tol_abs) +
+                     K(tol_rel) * (larger(f1, -f1) + larger(f2, -f2)));
+  const bool known = off < K(kInf);
+  const O low = to_order(known ? from_order(rank_by) - off : -K(kInf));
+  const O high = to_order(known ? from_order(rank_by) + off : K(kInf));
+  const O least = ~team_max<L>(kept && live ? O(~low) : O(0));
+  const O most = team_max<L>(mine < a.n_groups && !kept && live ? high : O(0));
+  return least <= most;
 }
 
 // One token's choice. Lane s < top_k gets the expert of slot s in `id` (-1:
@@ -312,10 +321,10 @@ __device__ __forceinline__ bool choose(const RouteArgs &a, Order<K> (&key)[V],
   // a round's value against the one before; that of round L is in no lane
   const O before = __shfl_up(chosen, 1, L);
   if (lane > 0 && chosen != 0)
-    close |= too_close(K(from_order(before)), K(from_order(chosen)), 1, tol_abs,
+    close |= too_close(K(from_order(before)), K(from_order(chosen)), tol_abs,
                        tol_rel);
   if (a.top_k == L && lane == L - 1 && last != 0)
-    close |= too_close(K(from_order(chosen)), K(from_order(last)), 1, tol_abs,
+    close |= too_close(K(from_order(chosen)), K(from_order(last)), tol_abs,
                        tol_rel);
   return team_bits<L>(close) == 0;
 }

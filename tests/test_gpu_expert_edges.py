@@ -253,3 +253,55 @@ def test_layer_refuses_before_it_runs(cl):
         t = t.view(torch.uint8) if t.dtype == E4M3 else t
         assert torch.equal(t, b)
     assert m.out is y
+
+
+# ---------------------------------------------------- groups and far biases ----
+
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("E,G,far", [(64, 32, 1000.0), (64, 16, 1000.0),
+                                     (60, 20, 1000.0), (256, 32, 3000.0)])
+def test_groups_whose_two_values_cancel(cl, E, G, far, sigmoid):
+    """Groups rank by the sum of two values of some +far and -far, each of which is
+    held to 2^-24 of far, so that ranks a thousandth apart may be in the wrong order
+    in fp32. Few and many tokens; chosen as 64 bits choose."""
+    T, k, S = 60_000, 4, E // G
+    l = randn(T, E, seed=E)
+    bias = randn(E, seed=G, std=0.02) - 4 * far
+    bias[0::S] += 5 * far
+    bias[1::S] += 3 * far
+    s = torch.sigmoid(l.double()) if sigmoid else torch.softmax(l.double(), 1)
+    v = s + bias.double()
+    rank = v.view(T, G, S)[:, :, :2].sum(2)
+    kept = torch.sort(rank, dim=1, descending=True, stable=True).indices[:, :5]
+    out = torch.ones(T, G, dtype=torch.bool).scatter_(1, kept, False)
+    v = v.masked_fill(out.repeat_interleave(S, 1), -math.inf)
+    expect = torch.sort(v, dim=1, descending=True, stable=True).indices[:, :k]
+    l, bias = l.to(DEV), bias.to(DEV)
+    for n in (T, 4000):
+        ids = torch.full((T, k), -7, dtype=torch.int32, device=DEV)
+        w = torch.empty(T, k, device=DEV)
+        for at in range(0, T, n):
+            cl.route_t(l[at:at + n], ids[at:at + n], w[at:at + n], bias=bias,
+                       groups=G, top_groups=5, group_top_two=True,
+                       sigmoid=sigmoid)
+        assert torch.equal(ids.cpu().long(), expect)
+
+
+@pytest.mark.parametrize("T", [1, 5000])
+def test_group_sums_past_fp32(cl, T):
+    """Two finite biases whose sum no float holds."""
+    l = torch.zeros(T, 12, device=DEV)
+    b = torch.tensor([2e38, 2.1e38, 0, 0, 3e38, 2.9e38, 0, 0, -3e38, -2e38,
+                      -3.1e38, -2.2e38], device=DEV)
+    ids = torch.full((T, 2), -7, dtype=torch.int32, device=DEV)
+    w = torch.empty(T, 2, device=DEV)
+    cl.route_t(l, ids, w, bias=b, groups=3, top_groups=1, group_top_two=True)
+    assert (ids == torch.tensor([4, 5], device=DEV)).all()
+    b = b - 0.0
+    b[:8] = torch.tensor([-3e38, -2.9e38, -3.1e38, -3.2e38] * 2)
+    b[4] = -2.8e38
+    b[8:] = b[0]
+    # sums -5.9e38, -5.7e38, -6e38; of the first two groups -2.8e38 is the highest,
+    # then -2.9e38, which experts 1 and 5 have
+    cl.route_t(l, ids, w, bias=b, groups=3, top_groups=2, group_top_two=True)
+    assert (ids == torch.tensor([4, 1], device=DEV)).all()
