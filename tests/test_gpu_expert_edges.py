@@ -305,3 +305,23 @@ def test_group_sums_past_fp32(cl, T):
     # then -2.9e38, which experts 1 and 5 have
     cl.route_t(l, ids, w, bias=b, groups=3, top_groups=2, group_top_two=True)
     assert (ids == torch.tensor([4, 1], device=DEV)).all()
+
+
+@pytest.mark.parametrize("E", [64, 256, 1024])
+def test_close_softmax_scores_beside_a_large_one(cl, E):
+    """One score ahead of many that are all but equal, where the sum's own error is
+    the largest: scores some 2^-20 of themselves apart, with biases that order
+    them by halves of that. Chosen as 64 bits choose, few and many tokens."""
+    T, k = 4200, 7
+    l = randn(T, E, seed=E) * 2.0 ** -20
+    l[:, 3] = torch.linspace(0, 11, T)
+    bias = randn(E, seed=1) * 2.0 ** -21 / E
+    v = torch.softmax(l.double(), 1) + bias.double()
+    expect = torch.sort(v, dim=1, descending=True, stable=True).indices[:, :k]
+    l, bias = l.to(DEV), bias.to(DEV)
+    for n in (T, 600):
+        ids = torch.full((T, k), -7, dtype=torch.int32, device=DEV)
+        w = torch.empty(T, k, device=DEV)
+        for at in range(0, T, n):
+            cl.route_t(l[at:at + n], ids[at:at + n], w[at:at + n], bias=bias)
+        assert torch.equal(ids.cpu().long(), expect)
