@@ -45,12 +45,19 @@ constexpr float kInf = __builtin_inff();
 //            s (1 - s) |l| <= 0.28, and the sum and the reciprocal are off by 1.5
 //            ulp: (0.25 + 1.5 * 0.28 + 1.5) 2^-23
 //   softmax  of the largest score p. The exponential of x <= 0 by (1 + 1.5 |x|) e^x <=
-//            1.08 of p; the sum by its exponentials', weighted by the scores, 1 + 1.5
-//            times a mean |x| that is at most 4.5 (one score ahead of 1023 equal ones),
-//            7.8, and by its additions (16 in a lane, 6 steps), 22 half ulps; the
-//            reciprocal and the product by 1.5: (1.08 + 7.8 + 11 + 1.5) p 2^-23
+//            1.08 of p; the reciprocal of the sum and the product by 1.5; the sum by its
+//            V + log2 L additions (V in a lane, then the team's steps), half an ulp
+//            each, and by its exponentials', weighted by the scores: 1 + 1.5 times the
+//            mean |x|. That is the entropy and the largest score's logarithm, the most
+//            for one of n experts ahead of equal ones: t - 1 with (n - 1) e^-t = t - 1.
 // and the bias's addition by half an ulp of the value.
-constexpr float kTolSigmoid = 3 * 0x1p-23f, kTolSoftmax = 22 * 0x1p-23f;
+constexpr float kTolSigmoid = 3 * 0x1p-23f;
+template <int V, int L>
+constexpr float softmax_tol() {
+  constexpr int n = V * L, steps = V + (L == 64 ? 6 : 4);
+  constexpr float mean = n <= 64 ? 2.4f : n <= 128 ? 2.9f : n <= 256 ? 3.4f : 4.5f;
+  return (1.08f + 1.5f + 0.5f * steps + 1 + 1.5f * mean) * 0x1p-23f;
+}
 constexpr float kTolRel = 0x1p-23f;
 
 __device__ __forceinline__ float exp_of(float x) {
@@ -352,7 +359,7 @@ __device__ __forceinline__ float values_of(const RouteArgs &a,
       sum += v[j];
     }
     sum = one_over(team_sum<L>(sum));  // the largest score
-    tol = kTolSoftmax * float(sum);
+    tol = softmax_tol<V, L>() * float(sum);
 #pragma unroll
     for (int j = 0; j < V; ++j) v[j] *= sum;
   }
