@@ -155,13 +155,6 @@ __device__ __forceinline__ O team_lane(O x, uint32_t i) {
     return __shfl(x, int(i), L);
 }
 
-// the team's first lane with p; 0 where there is none
-template <int L>
-__device__ __forceinline__ uint32_t team_first(bool p) {
-  const uint64_t who = team_bits<L>(p);
-  return who ? uint32_t(__builtin_ctzll(who)) : 0u;
-}
-
 // Whether groups of S experts are whole lanes of a row, 1, 2, 4 ... 16 of them.
 __device__ inline bool groups_in_row(uint32_t S, uint32_t V) {
   const uint32_t lanes = S / V;
@@ -481,13 +474,19 @@ __global__ void __launch_bounds__(64 * kWaves)
 //   sigmoid normalised   d_i = w_i (1 - s_i) (g_i - sum_j w_j g_j / c)
 //   sigmoid              d_i = c s_i (1 - s_i) g_i
 // (d_i for the chosen; 0 elsewhere). Only the plain softmax reads the whole
-// row. 1 - s is computed as the sigmoid of -l: subtracted from 1, an s close to it
-// leaves nothing (l = 16: 6% off, from 17 on 0). So it is with the largest chosen
-// score m of a softmax, which alone can near 1 or w_m = c: what it takes from itself is
-// left out on both sides,
+// row. 1 - s is computed beside s: subtracted from 1, an s close to it leaves nothing (l
+// = 16: 6% off, from 17 on 0). So it is with the largest share m, which
+// alone can near 1: what it takes from itself is left out on both sides,
 //   g_m - sum_j w_j g_j / c  =  g_m (1 - w_m / c) - sum_{j != m} w_j g_j / c
-// with 1 - w_m / c as the sum of the others' (of all others' scores where the weights
-// are not renormalised).
+// with 1 - w_m / c as the sum of the others' shares (of all other experts' scores where
+// weights are not renormalised). An m that is named twice has the other slot among them.
+// s and 1 - s of a sigmoid from the exponential that does not grow
+__device__ __forceinline__ void sigmoid_of(float l, float &s, float &off) {
+  const float e = expf(-fabsf(l)), large = 1.0f / (1.0f + e);
+  s = l >= 0 ? large : e * large;
+  off = l >= 0 ? e * large : large;
+}
+
 template <typename T, int V, int L>
 __global__ void __launch_bounds__(64 * kWaves)
     route_backward_kernel(RouteBackArgs a, bool vec, bool vec_out) {
@@ -513,63 +512,59 @@ __global__ void __launch_bounds__(64 * kWaves)
   }
   const float mine = chosen ? T::to_float(row[id]) : -kInf;
   float d = 0;  // of this lane's slot
-  float l[V], spread = 0, top = 0, sum = 1, top_d = 0;
-  int top_id = -1;  // whole: the largest chosen score's expert
+  float l[V], spread = 0, sum = 1;
+  int top_id = -1;  // whole: the expert of the largest score, if it is chosen
   const bool whole = !sigmoid && !normal;
-  float high = -kInf;
-  uint32_t m = 0;  // the largest chosen logit's slot
-  if (whole || normal) {
-    high = from_order(team_max<L>(to_order(mine)));
-    m = team_first<L>(chosen && mine == high);
-  }
   if (whole) {
     load_logits<T, V>(row, a.n_experts, vec, lane, l);
-    top = -kInf;
+    float top = -kInf;
 #pragma unroll
     for (int j = 0; j < V; ++j) top = l[j] > top || l[j] != l[j] ? l[j] : top;
     // a NaN stays the maximum's choice of no lane: the sum carries it instead
     top = from_order(team_max<L>(to_order(top == top ? top : -kInf)));
-    top_id = int(team_lane<L>(uint32_t(id), m));
+    const auto who =
+        team_bits<L>(chosen && mine == top && fabsf(top) < kInf);
+    const uint32_t m = who ? uint32_t(__builtin_ctzll(who)) : 0u;
+    if (who) top_id = int(team_lane<L>(uint32_t(id), m));
     float others = 0;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      l[j] = l[j] == -kInf ? 0.0f : expf(l[j] - top);
-      others += int(lane * V + j) == top_id ? 0.0f : l[j];
+      const bool out = l[j] == -kInf || int(lane * V + j) == top_id;
+      l[j] = out ? 0.0f : expf(l[j] - top);
+      others += l[j];
     }
     others = team_sum<L>(others);
-    const float mine_p = chosen && mine != -kInf ? expf(mine - top) : 0.0f;
-    sum = others + team_lane<L>(mine_p, m);
-    const float p = sum != 0 ? mine_p / sum : 0.0f;
+    sum = others + (who ? 1.0f : 0.0f);  // e^0
+    const float p = chosen && sum != 0 ? expf(mine - top) / sum : 0.0f;
     d = p * g;
-    const float rest = team_sum<L>(lane == m ? 0.0f : d);
-    spread = rest + team_lane<L>(d, m);
-    top_d = team_lane<L>(p * (g * (others / sum) - rest), m);
-    if (lane == m) d = 0;  // all of it is in top_d
+    spread = team_sum<L>(d);
+    const bool is_top = who && lane == m;
+    const float rest = team_sum<L>(is_top ? 0.0f : d);
+    if (is_top) d = p * (g * (others / sum) - rest);
   } else if (normal) {
+    const float high = from_order(team_max<L>(to_order(mine)));
+    const auto who = team_bits<L>(chosen && mine == high);
+    const bool is_top = who && lane == uint32_t(__builtin_ctzll(who));
     const bool as_exp = !sigmoid || high <= -30.0f;
-    const float off = sigmoid ? 1.0f / (1.0f + expf(mine)) : 1.0f;  // 1 - s
+    float s = 0, off = 1;
+    if (sigmoid) sigmoid_of(mine, s, off);
     float p = 0;
-    if (chosen && high != -kInf)
-      p = as_exp ? expf(mine - high) : 1.0f / (1.0f + expf(-mine));
-    const float others = team_sum<L>(lane == m ? 0.0f : p);
-    const float all = others + team_lane<L>(p, m);
+    if (chosen && high != -kInf) p = as_exp ? expf(mine - high) : s;
+    const float all = team_sum<L>(p), others = team_sum<L>(is_top ? 0.0f : p);
     const float w = all == 0 ? 0.0f : p / all;
     const float wg = chosen ? w * g : 0.0f;
-    const float rest = team_sum<L>(lane == m ? 0.0f : wg);
-    const float mean = rest + team_lane<L>(wg, m);
+    const float mean = team_sum<L>(wg), rest = team_sum<L>(is_top ? 0.0f : wg);
     const float from_mean =
-        lane != m ? g - mean : all == 0 ? 0.0f : g * (others / all) - rest;
+        !is_top ? g - mean : all == 0 ? 0.0f : g * (others / all) - rest;
     d = chosen ? w * off * from_mean : 0.0f;
   } else {
-    const float s = 1.0f / (1.0f + expf(-mine));
-    const float off = 1.0f / (1.0f + expf(mine));  // 1 - s
+    float s, off;
+    sigmoid_of(mine, s, off);
     d = chosen ? s * off * g : 0.0f;
   }
   float o[V];
 #pragma unroll
-  for (int j = 0; j < V; ++j)
-    o[j] = !whole                           ? 0.0f
-           : int(lane * V + j) == top_id ? top_d : -(l[j] / sum) * spread;
+  for (int j = 0; j < V; ++j) o[j] = whole ? -(l[j] / sum) * spread : 0.0f;
   if (whole && !(sum > 0)) {  // every logit is -inf, or one is NaN
 #pragma unroll
     for (int j = 0; j < V; ++j) o[j] = sum != sum ? sum : 0.0f;
