@@ -343,7 +343,9 @@ int ciera_select(const double *gain, const double *mem, uint64_t count,
  * values and at least the row's length. Sizes that would need a launch of 2^32
  * threads or more are refused: 2^26 tokens or rows (of ciera_route and its gradient,
  * ciera_quantize_rows), 2^26 (token, slot) pairs (ciera_combine_backward) or pieces
- * of 512 values of tokens (ciera_combine), 2^24 tiles of 128 x 128 (the others). Device indices out of range are never
+ * of 512 values of tokens (ciera_combine), 2^24 tiles of 128 x 128 (the others; the
+ * products' kernels may take tiles in pairs of rows, an expert's for the gradients, and
+ * of columns, and count a missing neighbour). Device indices out of range are never
  * followed. Sums are held in fp32; every result is rounded to its type once, to
  * nearest even, and depends on the inputs alone (no atomic adds).
  *

@@ -42,7 +42,12 @@ constexpr uint64_t kMostCols = uint64_t(1) << 30;
 constexpr uint64_t kMostGroups = uint64_t(1) << 24;
 constexpr uint64_t kMostWaves = 4 * kMostGroups;
 bool ints_ok(const void *p) { return p && aligned(p, 4); }
-int status(hipError_t e) { return e == hipSuccess ? CIERA_OK : CIERA_EHIP; }
+// sizes whose tiles one launch does not hold are the launchers' to find
+int status(hipError_t e) {
+  return e == hipSuccess                      ? CIERA_OK
+         : e == hipErrorInvalidConfiguration ? CIERA_EINVAL
+                                              : CIERA_EHIP;
+}
 
 }  // namespace
 
@@ -226,7 +231,7 @@ int ciera_expert_matmul(const void *a, uint64_t a_stride,
       (!offsets && n_experts != 1))
     return CIERA_EINVAL;
   if (n_rows == 0 || n_out == 0) return CIERA_OK;
-  // tiles of 128 x 128; the kernel of few rows looks for itself
+  // tiles of 128 x 128, before they are paired
   if (((n_rows + 127) / 128 + n_experts) * ((n_out + 127) / 128) >= kMostGroups)
     return CIERA_EINVAL;
   if (!narrow_ok(a, a_stride, a_scales, a_scale_stride, depth) ||

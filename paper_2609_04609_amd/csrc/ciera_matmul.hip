@@ -323,6 +323,10 @@ __device__ __forceinline__ TilePlace tile_of_workgroup(uint32_t col_tiles) {
 inline uint64_t workgroups_of(uint64_t row_tiles, uint64_t col_tiles) {
   return (row_tiles / 2 * ((col_tiles + 1) / 2) + 7) / 8 * 32;
 }
+// whether one launch holds them
+inline bool launchable(uint64_t workgroups, uint64_t threads) {
+  return workgroups * threads >> 32 == 0;
+}
 
 // Grid: tiles of the result's columns, then of the experts' rows.
 template <typename S, typename T>
@@ -1139,9 +1143,10 @@ hipError_t matmul_shaped(const MatmulArgs &a, hipStream_t s) {
       !a.offsets ? 1 : a.n_rows < a.n_experts ? a.n_rows : a.n_experts;
   const uint32_t rt = uint32_t((a.n_rows + (S::TR - 1) * some) / S::TR);
   const uint32_t ct = uint32_t((a.n_out + S::TC - 1) / S::TC);
-  expert_matmul_kernel<S, T>
-      <<<dim3(uint32_t(workgroups_of((rt + 1) & ~1u, ct))), dim3(S::kThreads), 0, s>>>(
-          a, rt, ct, aligned_fours(a.out, a.out_stride, T::kBytes));
+  const uint64_t groups = workgroups_of((rt + 1) & ~1u, ct);
+  if (!launchable(groups, S::kThreads)) return hipErrorInvalidConfiguration;
+  expert_matmul_kernel<S, T><<<dim3(uint32_t(groups)), dim3(S::kThreads), 0, s>>>(
+      a, rt, ct, aligned_fours(a.out, a.out_stride, T::kBytes));
   return hipGetLastError();
 }
 
@@ -1261,10 +1266,11 @@ template <typename S, typename T>
 hipError_t grad_shaped(const WeightGradArgs &a, hipStream_t s) {
   const uint32_t rt = uint32_t((a.n_out + S::TR - 1) / S::TR);
   const uint32_t ct = uint32_t((a.n_cols + S::TC - 1) / S::TC);
-  weight_grad_kernel<S, T>
-      <<<dim3(uint32_t(workgroups_of(uint64_t(a.n_experts) * ((rt + 1) & ~1u), ct))),
-         dim3(S::kThreads), 0, s>>>(
-          a, rt, ct, aligned_fours(a.d_w, a.n_cols, T::kBytes));
+  const uint64_t groups =
+      workgroups_of(uint64_t(a.n_experts) * ((rt + 1) & ~1u), ct);
+  if (!launchable(groups, S::kThreads)) return hipErrorInvalidConfiguration;
+  weight_grad_kernel<S, T><<<dim3(uint32_t(groups)), dim3(S::kThreads), 0, s>>>(
+      a, rt, ct, aligned_fours(a.d_w, a.n_cols, T::kBytes));
   return hipGetLastError();
 }
 
