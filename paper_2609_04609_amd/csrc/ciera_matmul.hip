@@ -1183,16 +1183,23 @@ bool many_tiles(uint64_t rows, uint64_t cols) {
 template <typename T, int FR, int SPLIT>
 hipError_t few_split(const MatmulArgs &a, uint32_t tiles, hipStream_t s) {
   const uint32_t groups = uint32_t((a.n_out + 64 / SPLIT - 1) / (64 / SPLIT));
-  if (uint64_t(tiles) * groups * 256 >> 32) return hipErrorInvalidConfiguration;
   few_rows_kernel<T, FR, SPLIT><<<dim3(tiles * groups), dim3(256), 0, s>>>(
       a, groups, aligned_fours(a.out, a.out_stride, T::kBytes));
   return hipGetLastError();
 }
+// rows of tiles of few_rows with that many fragments
+uint64_t few_tiles(const MatmulArgs &a, uint64_t experts, uint64_t fragments) {
+  return (a.n_rows + (16 * fragments - 1) * experts) / (16 * fragments);
+}
+// Whether one launch holds them. More than one wave share 16 columns only where that
+// makes few waves, so columns that are not shared are what counts.
+bool few_launchable(const MatmulArgs &a, uint64_t experts, uint64_t fragments) {
+  return launchable(few_tiles(a, experts, fragments) * ((a.n_out + 63) / 64), 256);
+}
 // As many parts of the depth as give every CU 16 waves, of four blocks or more.
 template <typename T, int FR>
 hipError_t few_rows(const MatmulArgs &a, uint64_t experts, hipStream_t s) {
-  const uint32_t tiles =
-      uint32_t((a.n_rows + (16 * FR - 1) * experts) / (16 * FR));
+  const uint32_t tiles = uint32_t(few_tiles(a, experts, FR));
   const uint64_t waves = tiles * ((a.n_out + 15) / 16);
   if (waves >= 4096 || a.depth <= 512) return few_split<T, FR, 1>(a, tiles, s);
   if (waves >= 2048 || a.depth <= 1024) return few_split<T, FR, 2>(a, tiles, s);
@@ -1247,8 +1254,8 @@ hipError_t matmul_typed(const MatmulArgs &a, hipStream_t s) {
       stream_fits(a.a_stride, a.b_stride, a.a_scale_stride, a.b_scale_stride,
                   a.out, a.out_stride, a.n_out);
   const int few = few_fragments(a, experts, T::kBytes == 4, streams);
-  if (few == 1) return few_rows<T, 1>(a, experts, s);
-  if (few == 4) return few_rows<T, 4>(a, experts, s);
+  if (few != 0 && few_launchable(a, experts, uint64_t(few)))
+    return few == 1 ? few_rows<T, 1>(a, experts, s) : few_rows<T, 4>(a, experts, s);
   if constexpr (T::kBytes == 2) {
     if (streams) {
       const ProductStream what{

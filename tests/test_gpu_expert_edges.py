@@ -325,3 +325,31 @@ def test_close_softmax_scores_beside_a_large_one(cl, E):
         for at in range(0, T, n):
             cl.route_t(l[at:at + n], ids[at:at + n], w[at:at + n], bias=bias)
         assert torch.equal(ids.cpu().long(), expect)
+
+
+# ------------------------------------------------------------------- sizes ----
+
+def test_few_rows_of_wide_weights(cl):
+    """131 GB of weights, for whose columns the kernel of few rows would need 2^32
+    threads and more: another takes them."""
+    if torch.cuda.get_device_properties(0).total_memory < 200 << 30:
+        pytest.skip("less than 200 GiB of memory")
+    E, N, D, P = 1024, 1_000_003, 128, 2048
+    w = torch.zeros(E, N, D, dtype=torch.uint8, device=DEV)
+    g = torch.Generator().manual_seed(1)
+    last = torch.randint(-8, 9, (300, D), generator=g).float()
+    w[-1, -300:] = last.to(E4M3).view(torch.uint8).to(DEV)
+    a = torch.randint(-8, 9, (P, D), generator=g).float()
+    sa = torch.full((P, 4), 127, dtype=torch.uint8, device=DEV)
+    sb = torch.full((E, -(-N // 128), 4), 127, dtype=torch.uint8, device=DEV)
+    off = torch.arange(0, P + 1, 2, dtype=torch.int32)  # two rows an expert
+    out = torch.full((P, N), 7.0, dtype=torch.bfloat16, device=DEV)
+    cl.expert_matmul_t(a.to(E4M3).to(DEV), sa, w.view(E4M3), sb, off.to(DEV),
+                       out)
+    expect = (a[-2:] @ last.t()).bfloat16()  # whole numbers below 2^24
+    assert torch.equal(out[-2:, -300:].cpu(), expect)
+    assert (out[-2:, :-300] == 0).all()
+    for rows in out[:-2].split(256):
+        assert not rows.any()
+    del w, out, rows
+    torch.cuda.empty_cache()
