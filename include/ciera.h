@@ -418,7 +418,8 @@ uint64_t ciera_plan_workspace_bytes(uint64_t n_tokens, uint32_t top_k,
 
 /* The (token, slot) pairs, numbered token * top_k + slot, sorted by expert; those
  * of one expert keep their order. Experts are first_expert ... first_expert +
- * n_experts - 1 (those that this rank holds); pairs of other ids are left out.
+ * n_experts - 1 (those that this rank holds, all below 2^31); pairs of other ids are
+ * left out.
  *   offsets   [n_experts + 1] int32: rows of expert e are offsets[e] ...
  *             offsets[e + 1] - 1, offsets[0] = 0
  *   source    [n_tokens * top_k] int32: the pair behind each row; -1 from row

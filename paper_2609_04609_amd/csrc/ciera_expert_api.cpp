@@ -124,7 +124,8 @@ int ciera_route_plan(const int32_t *expert_ids, uint64_t n_tokens,
                      uint64_t workspace_bytes, hipStream_t stream) {
   CallScope scope;
   const uint64_t need = ciera_plan_workspace_bytes(n_tokens, top_k, n_experts);
-  if (need == 0 || first_expert >= kMost || !ints_ok(offsets))
+  // the last expert is an int32 too: differences of negative ids stay outside
+  if (need == 0 || first_expert > kMost - n_experts || !ints_ok(offsets))
     return CIERA_EINVAL;
   if (n_tokens > 0 && (!ints_ok(expert_ids) || !ints_ok(source) ||
                        !ints_ok(position) || !ints_ok(workspace)))

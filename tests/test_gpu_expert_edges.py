@@ -353,3 +353,19 @@ def test_few_rows_of_wide_weights(cl):
         assert not rows.any()
     del w, out, rows
     torch.cuda.empty_cache()
+
+
+def test_plan_of_the_last_experts(cl):
+    """Ids up to 2^31 - 1, beside negative ones whose difference wraps."""
+    E, first = 8, 2 ** 31 - 8
+    ids = torch.tensor([[2 ** 31 - 1, -1], [-2 ** 31, 2 ** 31 - 8],
+                        [-2 ** 31 + 3, 2 ** 31 - 2], [0, 2 ** 31 - 8]])
+    off = torch.full((E + 1,), -9, dtype=torch.int32, device=DEV)
+    src = torch.full((8,), -9, dtype=torch.int32, device=DEV)
+    pos = torch.full((4, 2), -9, dtype=torch.int32, device=DEV)
+    cl.route_plan_t(ids.int().to(DEV), E, off, src, pos,
+                    cl.PlanWorkspace(4, 2, E), first_expert=first)
+    o, s, p = ref.plan(ids, E, first)
+    assert torch.equal(off.cpu().long(), o)
+    assert torch.equal(src.cpu().long(), s)
+    assert torch.equal(pos.cpu().long(), p)

@@ -32,3 +32,11 @@ def test_weight_grad(cl, dtype, E, N, C):
 def test_products(cl, dtype, R, N):
     assert cl.ciera_expert_matmul(P, 128, P, 4, R, P, 128, P, 4, 1, N, 128, 0,
                                   P, dtype, N, 0) == cl.EINVAL
+
+
+def test_plan_of_experts_past_int32(cl):
+    """No id names them, and a negative id must not."""
+    need = cl.ciera_plan_workspace_bytes(10, 2, 64)
+    for first in ((1 << 31) - 63, (1 << 31) - 1):
+        assert cl.ciera_route_plan(P, 10, 2, first, 64, P, P, P, P, need,
+                                   0) == cl.EINVAL
