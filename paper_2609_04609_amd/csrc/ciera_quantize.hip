@@ -3,8 +3,8 @@
 // costs its read, half an instruction for the maximum and half a conversion, which
 // scales too. 16384 tokens of 2048 bf16 values to 8 rows each: 69 us for 340 MB; a
 // layer of 64 x 1024 x 2048 both ways round: 102 us for 540 MB; 40024 rows gathered
-// from 5003 tokens, by columns: 26 us for 82 MB written and 164 MB read, of which 20 MB
-// from memory and the rest from the L2s.
+// from 5003 tokens, by columns: 26 us for 82 MB written and 164 MB read, of which 51 MB
+// from memory (counted; tokens are 20 MB, met by several XCDs) and the rest from the L2s.
 #include <type_traits>
 
 #include "ciera_expert.h"
