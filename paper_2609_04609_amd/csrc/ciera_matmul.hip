@@ -590,10 +590,11 @@ struct Sums {
   uint32_t before[CIERA_MAX_EXPERTS + 1];
   uint32_t first[CIERA_MAX_EXPERTS], last[CIERA_MAX_EXPERTS];
 };
-// By one wave.
+// By one wave. Rows end at n_rows, and no expert counts more than `most`.
 __device__ __forceinline__ void sum_experts(Sums &s, const int32_t *offsets,
                                             uint32_t n_experts, uint32_t n_rows,
-                                            uint32_t log2_unit, uint32_t lane) {
+                                            uint32_t most, uint32_t log2_unit,
+                                            uint32_t lane) {
   uint32_t before = 0;
   for (uint32_t from = 0; from < n_experts; from += 64) {
     const uint32_t e = from + lane;
@@ -603,10 +604,10 @@ __device__ __forceinline__ void sum_experts(Sums &s, const int32_t *offsets,
       hi = offsets ? offset_of(offsets, e + 1, n_rows) : n_rows;
       if (hi < lo) hi = lo;
     }
+    const uint32_t rows = hi - lo < most ? hi - lo : most;
     uint32_t total;
     const uint32_t start =
-        before +
-        wave_prefix((hi - lo + (1u << log2_unit) - 1) >> log2_unit, total);
+        before + wave_prefix((rows + (1u << log2_unit) - 1) >> log2_unit, total);
     before += total;
     if (e < n_experts) {
       s.before[e] = start;
@@ -631,7 +632,8 @@ struct ProductStream {
   static constexpr bool kColBlocks = true;  // a scale for 128 of the columns
   __device__ __forceinline__ uint32_t n_cols() const { return uint32_t(a.n_out); }
   __device__ __forceinline__ void prepare(Sums &s, uint32_t lane) const {
-    sum_experts(s, a.offsets, a.n_experts, uint32_t(a.n_rows), 8, lane);
+    const uint32_t n = uint32_t(a.n_rows);
+    sum_experts(s, a.offsets, a.n_experts, n, n, 8, lane);
   }
   __device__ __forceinline__ Job job(const Sums &s, uint32_t t,
                                      uint32_t lane) const {
@@ -686,7 +688,7 @@ struct GradStream {
   __device__ __forceinline__ uint32_t n_cols() const { return uint32_t(a.n_cols); }
   __device__ __forceinline__ void prepare(Sums &s, uint32_t lane) const {
     // no expert has more rows than there are columns
-    sum_experts(s, a.offsets, a.n_experts, uint32_t(a.length), 7, lane);
+    sum_experts(s, a.offsets, a.n_experts, ~0u, uint32_t(a.length), 7, lane);
   }
   __device__ __forceinline__ Job job(const Sums &s, uint32_t t, uint32_t) const {
     Job j{0, 0, 0, 0, 0, 0, 4};
@@ -1080,24 +1082,22 @@ __global__ void __launch_bounds__(256, 1) stream_kernel(P what) {
 }
 
 // Where an expert's columns start and how many there are, in blocks of 128
-// rows.
+// rows; no expert has more rows than there are columns, `most`.
+__device__ __forceinline__ uint32_t blocks_of(const int32_t *offsets, uint32_t e,
+                                              uint32_t most) {
+  const uint32_t lo = offset_of(offsets, e, ~0u);
+  const uint32_t hi = offset_of(offsets, e + 1, ~0u);
+  const uint32_t rows = hi > lo ? hi - lo : 0;
+  return ((rows < most ? rows : most) + 127) / 128;
+}
 __device__ __forceinline__ void blocks_of_expert(const int32_t *offsets,
-                                                 uint32_t n_rows,
-                                                 uint32_t expert, uint32_t lane,
-                                                 uint32_t &start,
+                                                 uint32_t most, uint32_t expert,
+                                                 uint32_t lane, uint32_t &start,
                                                  uint32_t &blocks) {
   uint32_t sum = 0;
-  for (uint32_t e = lane; e < expert; e += 64) {
-    const uint32_t lo = offset_of(offsets, e, n_rows);
-    const uint32_t hi = offset_of(offsets, e + 1, n_rows);
-    sum += hi > lo ? (hi - lo + 127) / 128 : 0;
-  }
-  uint32_t total;
-  wave_prefix(sum, total);
-  start = total;
-  const uint32_t lo = offset_of(offsets, expert, n_rows);
-  const uint32_t hi = offset_of(offsets, expert + 1, n_rows);
-  blocks = hi > lo ? (hi - lo + 127) / 128 : 0;
+  for (uint32_t e = lane; e < expert; e += 64) sum += blocks_of(offsets, e, most);
+  wave_prefix(sum, start);
+  blocks = blocks_of(offsets, expert, most);
 }
 
 template <typename S, typename T>

@@ -56,6 +56,24 @@ def test_weight_grad_of_offsets_that_fall(cl, dtype, E, top):
         start += n
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_weight_grad_of_offsets_that_start_late(cl, dtype):
+    """The experts' columns alone, of rows that lie behind many others."""
+    N, C, counts = 24, 40, [100, 0, 200]
+    off = torch.tensor([5000] + counts).cumsum(0).int()
+    L = cl.ciera_columns_length(300, 3)
+    g = torch.Generator().manual_seed(3)
+    dy = torch.randint(-4, 5, (N, L), generator=g).float()
+    x = torch.randint(-4, 5, (C, L), generator=g).float()
+    one = torch.full((C, 8), 127, dtype=torch.uint8, device=DEV)
+    dw = torch.full((3, N, C), 9.0, dtype=dtype, device=DEV)
+    cl.expert_weight_grad_t(dy.to(E4M3).to(DEV), one[:N].contiguous(),
+                            x.to(E4M3).to(DEV), one, off.to(DEV), dw)
+    for e, part in enumerate((slice(0, 128), slice(0, 0), slice(128, 384))):
+        expect = dy[:, part] @ x[:, part].t()
+        assert torch.equal(dw[e].cpu(), expect.to(dtype)), e
+
+
 # ------------------------------------------------------- saturated scores ----
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16,
