@@ -55,6 +55,8 @@ class ExpertLayer:
         T, k, E, N, C = n_tokens, top_k, n_experts, n_out, n_in
         if min(T, k, E, N, C) < 1:
             raise ValueError("a layer needs tokens, experts and values")
+        if dtype not in ciera._WIDE:
+            raise ValueError(f"dtype is {dtype}")
         P = T * k
         self.T, self.k, self.E, self.N, self.C = T, k, E, N, C
         self.train, self.choice = train, choice

@@ -40,3 +40,16 @@ def test_plan_of_experts_past_int32(cl):
     for first in ((1 << 31) - 63, (1 << 31) - 1):
         assert cl.ciera_route_plan(P, 10, 2, first, 64, P, P, P, P, need,
                                    0) == cl.EINVAL
+
+
+@pytest.mark.parametrize("train", [False, True])
+def test_layer_of_a_type_without_kernels(cl, train):
+    import torch
+
+    from paper_2609_04609_amd.experts import ExpertLayer
+    with pytest.raises(ValueError, match="dtype is torch.float64"):
+        ExpertLayer(4, 2, 4, 16, 16, dtype=torch.float64, device="cpu",
+                    train=train)
+    m = ExpertLayer(4, 2, 4, 16, 16, dtype=torch.float16, device="cpu",
+                    train=train)
+    assert m.out.dtype == torch.float16
