@@ -48,15 +48,21 @@ class ExpertLayer:
     """``top_k`` of ``n_experts`` experts of [n_out, n_in] weights for
     ``n_tokens`` tokens of ``dtype``; ``choice`` are the keywords of
     ciera.route_t (sigmoid, normalize, scale, groups, ...). With ``train`` there
-    are buffers for backward() too."""
+    are buffers for backward() too; ``grad_dtype`` is the weights' gradients'
+    type, the layer's if None."""
 
     def __init__(self, n_tokens, top_k, n_experts, n_out, n_in,
-                 dtype=torch.bfloat16, device="cuda", train=True, **choice):
+                 dtype=torch.bfloat16, device="cuda", train=True,
+                 grad_dtype=None, **choice):
         T, k, E, N, C = n_tokens, top_k, n_experts, n_out, n_in
         if min(T, k, E, N, C) < 1:
             raise ValueError("a layer needs tokens, experts and values")
         if dtype not in ciera._WIDE:
             raise ValueError(f"dtype is {dtype}")
+        if grad_dtype is None:
+            grad_dtype = dtype
+        elif grad_dtype not in ciera._WIDE:
+            raise ValueError(f"grad_dtype is {grad_dtype}")
         P = T * k
         self.T, self.k, self.E, self.N, self.C = T, k, E, N, C
         self.train, self.choice = train, choice
@@ -92,7 +98,7 @@ class ExpertLayer:
         (_, _), (_, Ls) = ciera.quantized_shapes(1, L)
         self.dy_t, self.dy_t_scales = eight(N, L), scales(N, Ls)
         self.x_t, self.x_t_scales = eight(C, L), scales(C, Ls)
-        self.d_w = new(E, N, C)
+        self.d_w = new(E, N, C, dtype=grad_dtype)
         # the logits' gradient has their type, which need not be the tokens'
         room = new(T * E, dtype=f32)
         self._d_logits = {t: room.view(t)[:T * E].view(T, E)
@@ -122,8 +128,8 @@ class ExpertLayer:
 
     def backward(self, d_out, x, logits):
         """Gradient of the output that forward() gave for ``x`` and ``logits``
-        -> gradients of x, of the weights and of the logits, the first two of the
-        layer's type, the last of the logits'."""
+        -> gradients of x (of the layer's type), of the weights (of grad_dtype) and
+        of the logits (of their type)."""
         if not self.train:
             raise ValueError("a layer without train has no backward")
         _inputs((d_out, "d_out", (self.out.dtype,), (self.T, self.N)),

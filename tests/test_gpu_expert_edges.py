@@ -273,6 +273,43 @@ def test_layer_refuses_before_it_runs(cl):
     assert m.out is y
 
 
+@pytest.mark.parametrize("dtype,grad", [(torch.bfloat16, torch.float32),
+                                        (torch.float16, torch.float32),
+                                        (torch.float32, torch.bfloat16)])
+def test_layer_with_weight_gradients_of_another_type(cl, dtype, grad):
+    """Everything else has the bits of a layer without; the gradients are those of
+    the 8-bit operands that the layer left, off by a rounding of 2^-23 for each of n
+    sums (16-bit ones by the half step and 2^-10 of the products' sizes)."""
+    T, k, E, N, C = 90, 3, 5, 72, 136
+    args = [randn(T, C, seed=1).to(dtype), randn(T, E, seed=2).to(dtype),
+            randn(T, N, seed=3).to(dtype)]
+    x, l, g = (t.to(DEV) for t in args)
+    w = randn(E, N, C, seed=4).to(dtype).to(DEV)
+    runs = []
+    for o in (dict(grad_dtype=grad), dict()):
+        m = layer(T, k, E, N, C, dtype=dtype, normalize=True, **o)
+        m.load(w)
+        runs.append([m, m.forward(x, l)] + list(m.backward(g, x, l)))
+    (m, y, d_x, d_w, d_l), other = runs
+    assert d_w.dtype == grad and other[3].dtype == dtype
+    for a, b in ((y, other[1]), (d_x, other[2]), (d_l, other[4])):
+        assert torch.equal(a, b)
+    off, start = m.offsets.tolist(), 0
+    half = torch.finfo(grad).eps / 2
+    for e in range(E):
+        n = off[e + 1] - off[e]
+        end = start + -(-n // 128) * 128
+        at = slice(start // 128, end // 128)
+        a = ref.values(m.dy_t[:, start:end], m.dy_t_scales[:, at], 1, 128)
+        b = ref.values(m.x_t[:, start:end], m.x_t_scales[:, at], 1, 128)
+        size = a.abs() @ b.abs().t()
+        bound = half * (a @ b.t()).abs() + n * 2.0 ** -23 * size
+        if grad != torch.float32:
+            bound = bound + 2.0 ** -10 * size
+        assert ((d_w[e].double().cpu() - a @ b.t()).abs() <= bound).all()
+        start = end
+
+
 # ---------------------------------------------------- groups and far biases ----
 
 @pytest.mark.parametrize("sigmoid", [False, True])

@@ -53,3 +53,6 @@ def test_layer_of_a_type_without_kernels(cl, train):
     m = ExpertLayer(4, 2, 4, 16, 16, dtype=torch.float16, device="cpu",
                     train=train)
     assert m.out.dtype == torch.float16
+    with pytest.raises(ValueError, match="grad_dtype is torch.int32"):
+        ExpertLayer(4, 2, 4, 16, 16, device="cpu", train=train,
+                    grad_dtype=torch.int32)
